@@ -245,6 +245,61 @@ salad_status salad_gate_fwd(const void *x_t, const float *w_gate, float b_gate, 
 salad_status salad_gate_fwd_static(const void *x_t, const float *w_gate, float b_gate, int32_t B, int32_t N,
                                    int32_t D, int32_t dtype, float *s_out, void *hip_stream);
 
+/* ---- causal layers: window attention with sinks ------------------------------------------------
+ * The causal counterpart of the layer's sparse branch, for generation that streams token by token (or clip by clip) and for
+ * training it.  Query n of sample b stands at position p = kv_len[b] - q_len[b] + n, so that the last query is at the last key.
+ * It sees key j when
+ *     j <= p  and  (j > p - window  or  j < sinks):
+ * the `window` most recent keys, itself included, and the first `sinks` keys of the sequence.
+ *   out = softmax(scale q k^T) v over the keys it sees,   lse = log sum exp(scale q k^T)  (natural logarithm, fp32)
+ * A query that sees no key (p < 0) gets zeros and lse = -infinity.
+ *   q, out [B,H,Nq,d];  k, v [B,Hk,Nk,d], H a multiple of Hk: query head h reads key head h / (H / Hk).  d is 64 or 128.
+ *   q_lens, kv_lens   device int32 [B] or NULL (= Nq, Nk): the samples of a padded batch.  Query rows behind q_len and key rows
+ *                     behind kv_len are not read (they may hold anything, NaN included); rows of out, lse, dq behind q_len and
+ *                     of dk, dv behind kv_len are left as they were.  Values outside 0..Nq and 0..Nk are taken as the nearer end.
+ *   ring              0: position j is row j of k and v.  1: k and v are a rolling cache: row j for j < sinks, else
+ *                     sinks + (j - sinks) % (Nk - sinks).  kv_lens is then needed, counts all positions ever (up to 2^30), and
+ *                     Nk >= sinks + window + Nq - 1 is needed for every key that some query sees to be there still.
+ * A value that is not finite in a key or value row reaches the queries that see the row, and may reach queries close to them that
+ * do not (0 * NaN in a shared tile).
+ * bf16: matrix cores, fp32 accumulation, P (and dS) rounded to bf16 for the products.  fp32: fp32 matrix instructions.
+ * Results do not depend on what else runs: no atomics, the same bits for the same call. */
+typedef struct salad_window_params {
+    int32_t B, H, Hk, Nq, Nk, d;
+    int32_t dtype;              /* salad_dtype of all tensors but lse                               */
+    int32_t window, sinks;      /* window >= 1, sinks >= 0                                          */
+    int32_t ring;
+    float softmax_scale;        /* 0 selects 1/sqrt(d); not negative                                */
+    const void *q, *k, *v;      /* device, 16-byte aligned like every tensor here                   */
+    void *out;                  /* written by the forward call, read by the backward call           */
+    float *lse;                 /* device [B,H,Nq]: written by the forward call (NULL: not wanted), read by the backward call */
+    const int32_t *q_lens, *kv_lens;
+    const void *dout;           /* backward only: [B,H,Nq,d]                                        */
+    void *dq, *dk, *dv;         /* backward only, shapes of q, k, v; written whole (up to the lengths) */
+    void *workspace;            /* device, 256-byte aligned, salad_window_attn_workspace_bytes(); NULL where that is 0 */
+    size_t workspace_bytes;
+    void *hip_stream;
+} salad_window_params;
+
+/* Device scratch of a call; reads the shape, dtype, window, sinks and ring only.  0 if none is needed or the shape is invalid.
+ * Nothing in it has to be set or kept between calls, but calls that may overlap must not share one. */
+size_t salad_window_attn_workspace_bytes(const salad_window_params *p, int32_t backward);
+
+/* Any Nq: a prompt, a chunk of one behind a cache, or single tokens (the keys are then cut into shares for the whole chip). */
+salad_status salad_window_attn_fwd(const salad_window_params *p);
+
+/* Gradients of sum(out * dout) with respect to q, k and v; the heads of a group add up in dk and dv.  out and lse are the forward
+ * call's.  ring must be 0. */
+salad_status salad_window_attn_bwd(const salad_window_params *p);
+
+/* New tokens into a cache: token n < q_len of sample b becomes position kv_len[b] - q_len[b] + n of k_cache, v_cache [B,Hk,Nk,d] (rows
+ * as above, with the same ring and sinks); k_new, v_new [B,Hk,Nq,d].  kv_lens is the length with the new tokens, as the attention
+ * call behind it takes it.  Positions that a later token of the same call takes the row of, and positions outside a cache
+ * that is not a ring, are left out. */
+salad_status salad_window_cache_append(const void *k_new, const void *v_new, void *k_cache, void *v_cache, int32_t B, int32_t Hk,
+                                       int32_t Nq, int32_t Nk, int32_t d, int32_t dtype, int32_t sinks, int32_t ring,
+                                       const int32_t *q_lens, const int32_t *kv_lens, void *hip_stream);
+
 /* ---- per-kernel timing ----------------------------------------------------------------------- */
 
 typedef struct salad_kernel_times {

@@ -15,7 +15,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libsalad.so")
 SOURCES = ["salad_api.hip", "mask_gate_finalize.hip", "linear_state.hip", "sparse_attn.hip", "sparse_attn_f32.hip",
-           "sparse_attn_v2.hip", "sparse_attn_v5.hip", "linear_apply.hip", "proj.hip", "topk.hip"]
+           "sparse_attn_v2.hip", "sparse_attn_v5.hip", "linear_apply.hip", "proj.hip", "topk.hip",
+           "causal_api.hip", "window_attn.hip", "window_grad.hip"]
 
 SALAD_OK, SALAD_EINVAL, SALAD_ENOTSUP, SALAD_ENOSPC, SALAD_EHIP = range(5)
 SALAD_F32, SALAD_BF16 = 0, 1
@@ -26,7 +27,8 @@ SALAD_FLAG_UNFUSED_EPILOGUE = 1
 EXPORTS = ["salad_last_error", "salad_kept_from_sparsity", "salad_block_mask_nnz", "salad_block_mask",
            "salad_block_mask_nnz_mode", "salad_block_mask_mode",
            "salad_tile_lists_bytes", "salad_tile_lists", "salad_proj_pack_bytes", "salad_proj_pack", "salad_fwd_workspace_bytes", "salad_sparse_linear_attn_fwd", "salad_linear_state_fwd",
-           "salad_gate_fwd", "salad_gate_fwd_static", "salad_timing_enable", "salad_timing_read", "salad_tune"]
+           "salad_gate_fwd", "salad_gate_fwd_static", "salad_timing_enable", "salad_timing_read", "salad_tune",
+           "salad_window_attn_workspace_bytes", "salad_window_attn_fwd", "salad_window_attn_bwd", "salad_window_cache_append"]
 
 
 class SaladError(RuntimeError):
@@ -71,6 +73,13 @@ class FwdParams(C.Structure):
         ("tile_lists", C.c_void_p),
         ("w_proj_packed", C.c_void_p),
     ]
+
+
+class WindowParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hk", "Nq", "Nk", "d", "dtype", "window", "sinks", "ring")] + [
+        ("softmax_scale", C.c_float)] + [
+        (n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "q_lens", "kv_lens", "dout", "dq", "dk", "dv", "workspace")] + [
+        ("workspace_bytes", C.c_size_t), ("hip_stream", C.c_void_p)]
 
 
 class KernelTimes(C.Structure):
@@ -157,6 +166,12 @@ def lib() -> C.CDLL:
         L.salad_timing_enable.argtypes = [C.c_int32]
         L.salad_timing_read.restype = C.c_int
         L.salad_timing_read.argtypes = [C.POINTER(KernelTimes), C.c_int32]
+        L.salad_window_attn_workspace_bytes.restype = C.c_size_t
+        L.salad_window_attn_workspace_bytes.argtypes = [C.POINTER(WindowParams), C.c_int32]
+        for f in (L.salad_window_attn_fwd, L.salad_window_attn_bwd):
+            f.restype, f.argtypes = C.c_int, [C.POINTER(WindowParams)]
+        L.salad_window_cache_append.restype = C.c_int
+        L.salad_window_cache_append.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 8 + [C.c_void_p] * 3
         L.salad_tune.restype = C.c_int
         L.salad_tune.argtypes = [C.c_char_p, C.c_int32]
         _lib = L
@@ -408,3 +423,154 @@ def salad_timing_read(reset: bool = True) -> KernelTimes:
 
 def salad_tune(key: str, value: int) -> None:
     _check(lib().salad_tune(key.encode(), value))
+
+
+# ---------------------------------------------------------------------------------------------
+# causal layers: window attention with sinks
+# ---------------------------------------------------------------------------------------------
+
+class CausalWorkspace:
+    """Scratch for the calls of a causal layer on one stream.  It grows to the largest call that it is passed to (or to `nbytes` at
+    once); a call that is captured into a graph has to find it large enough, so run the call once before, and keep the object as
+    long as the graph.  Calls that may overlap must not share one."""
+
+    def __init__(self, nbytes: int = 0, device=None):
+        self.buf, self.kept, self.ptr, self.bytes = None, [], None, 0
+        if nbytes:
+            import torch
+            self._grow(int(nbytes), torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device))
+
+    def _grow(self, need: int, device) -> None:
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError(f"the workspace has {self.bytes} bytes and a captured call needs {need}: run the call once before its capture")
+        if self.buf is not None:
+            self.kept.append(self.buf)              # graphs that were captured with it go on using it
+        self.buf = torch.empty(need + 256, dtype=torch.uint8, device=device)
+        self.ptr, self.bytes = (self.buf.data_ptr() + 255) & ~255, need
+
+    def room(self, need: int, device):
+        """(pointer, bytes) for a call that needs `need` bytes."""
+        if need > self.bytes:
+            self._grow(need, device)
+        elif self.buf is not None and self.buf.device != device:
+            raise ValueError(f"the workspace is on {self.buf.device}, the call's tensors are on {device}")
+        return self.ptr, self.bytes
+
+
+def _call_on(device, call):
+    """Runs call() with `device` current: launches go to it and to its current stream, whatever device the thread is on."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def _tensor(name, t, shape, dtype, device, optional=False):
+    """Checks a tensor argument; its pointer, or None."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is missing")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def _query(q):
+    if q.dim() != 4:
+        raise ValueError(f"q has {q.dim()} dimensions, expected [B, H, N, d]")
+    if not q.is_cuda:
+        raise ValueError("q is not on a GPU: there is no CPU path")
+    return _dtype_code(q)
+
+
+def _window_params(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale):
+    import torch
+    p = WindowParams()
+    p.dtype = _query(q)
+    B, H, Nq, d = q.shape
+    if k.dim() != 4:
+        raise ValueError(f"k has {k.dim()} dimensions, expected [B, Hk, Nk, d]")
+    Hk, Nk = k.shape[1], k.shape[2]
+    p.B, p.H, p.Hk, p.Nq, p.Nk, p.d = B, H, Hk, Nq, Nk, d
+    p.window, p.sinks, p.ring, p.softmax_scale = int(window), int(sinks), int(bool(ring)), softmax_scale
+    p.q = _tensor("q", q, q.shape, q.dtype, q.device)
+    p.k = _tensor("k", k, (B, Hk, Nk, d), q.dtype, q.device)
+    p.v = _tensor("v", v, (B, Hk, Nk, d), q.dtype, q.device)
+    p.q_lens = _tensor("q_lens", q_lens, (B,), torch.int32, q.device, optional=True)
+    p.kv_lens = _tensor("kv_lens", kv_lens, (B,), torch.int32, q.device, optional=True)
+    return p
+
+
+def _with_workspace(p, need: int, workspace, device):
+    ws = workspace
+    if need:
+        ws = CausalWorkspace() if workspace is None else workspace
+        if workspace is None:
+            import torch
+            ws.buf = torch.empty(need + 256, dtype=torch.uint8, device=device)      # one call's own, also under capture
+            ws.ptr, ws.bytes = (ws.buf.data_ptr() + 255) & ~255, need
+        p.workspace, p.workspace_bytes = ws.room(need, device)
+    p.hip_stream = _stream()
+    return ws
+
+
+def salad_window_attn_fwd(q, k, v, window: int, sinks: int = 0, *, q_lens=None, kv_lens=None, ring: bool = False, softmax_scale: float = 0.0,
+                          out=None, lse=None, workspace: Optional[CausalWorkspace] = None):
+    """Causal attention over the `window` most recent keys and the first `sinks`: q [B,H,Nq,d], k and v [B,Hk,Nk,d] -> out [B,H,Nq,d].
+    Pass `lse` (fp32 [B,H,Nq]) to have the rows' log-sum-exp, which the backward call takes.  See include/salad.h for positions,
+    lengths and the rolling cache (`ring`)."""
+    import torch
+    p = _window_params(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale)
+
+    def call():
+        o = torch.empty_like(q) if out is None else out
+        p.out = _tensor("out", o, q.shape, q.dtype, q.device)
+        p.lse = _tensor("lse", lse, q.shape[:3], torch.float32, q.device, optional=True)
+        keep = _with_workspace(p, int(lib().salad_window_attn_workspace_bytes(C.byref(p), 0)), workspace, q.device)
+        _check(lib().salad_window_attn_fwd(C.byref(p)))
+        del keep
+        return o
+    return _call_on(q.device, call)
+
+
+def salad_window_attn_bwd(q, k, v, out, lse, dout, window: int, sinks: int = 0, *, q_lens=None, kv_lens=None, softmax_scale: float = 0.0,
+                          dq=None, dk=None, dv=None, workspace: Optional[CausalWorkspace] = None):
+    """Gradients (dq, dk, dv) of sum(out * dout) for salad_window_attn_fwd with the same arguments; out and lse are that call's."""
+    import torch
+    p = _window_params(q, k, v, window, sinks, q_lens, kv_lens, False, softmax_scale)
+
+    def call():
+        p.out = _tensor("out", out, q.shape, q.dtype, q.device)
+        p.lse = _tensor("lse", lse, q.shape[:3], torch.float32, q.device)
+        p.dout = _tensor("dout", dout, q.shape, q.dtype, q.device)
+        g = [torch.empty_like(x) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
+        p.dq, p.dk, p.dv = (_tensor(n, x, y.shape, q.dtype, q.device) for n, x, y in zip(("dq", "dk", "dv"), g, (q, k, v)))
+        keep = _with_workspace(p, int(lib().salad_window_attn_workspace_bytes(C.byref(p), 1)), workspace, q.device)
+        _check(lib().salad_window_attn_bwd(C.byref(p)))
+        del keep
+        return tuple(g)
+    return _call_on(q.device, call)
+
+
+def salad_window_cache_append(k_new, v_new, k_cache, v_cache, sinks: int, kv_lens, *, q_lens=None, ring: bool = True) -> None:
+    """New tokens [B,Hk,Nq,d] into the rows of their positions in a cache [B,Hk,Nk,d]; kv_lens (device int32 [B]) is the length with them,
+    as the attention call behind takes it."""
+    import torch
+    code = _query(k_new)
+    B, Hk, Nq, d = k_new.shape
+    if k_cache.dim() != 4:
+        raise ValueError(f"k_cache has {k_cache.dim()} dimensions, expected [B, Hk, Nk, d]")
+    Nk, dev, dt = k_cache.shape[2], k_new.device, k_new.dtype
+    ptrs = [_tensor("k_new", k_new, k_new.shape, dt, dev), _tensor("v_new", v_new, k_new.shape, dt, dev),
+            _tensor("k_cache", k_cache, (B, Hk, Nk, d), dt, dev), _tensor("v_cache", v_cache, (B, Hk, Nk, d), dt, dev)]
+    lens = [_tensor("q_lens", q_lens, (B,), torch.int32, dev, optional=True), _tensor("kv_lens", kv_lens, (B,), torch.int32, dev)]
+    _call_on(dev, lambda: _check(lib().salad_window_cache_append(*ptrs, B, Hk, Nq, Nk, d, code, int(sinks), int(bool(ring)), *lens, _stream())))

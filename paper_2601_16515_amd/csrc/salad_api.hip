@@ -17,12 +17,13 @@
 
 #include "../../include/salad.h"
 #include "salad_internal.h"
+#include "salad_status.h"
 
 using namespace salad;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
+namespace salad {
 
 salad_status fail(salad_status st, const char *fmt, ...)
 {
@@ -37,6 +38,10 @@ salad_status hip_fail(hipError_t e, const char *what)
 {
     return fail(SALAD_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace salad
+
+namespace {
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
