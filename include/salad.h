@@ -300,6 +300,48 @@ salad_status salad_window_cache_append(const void *k_new, const void *v_new, voi
                                        int32_t Nq, int32_t Nk, int32_t d, int32_t dtype, int32_t sinks, int32_t ring,
                                        const int32_t *q_lens, const int32_t *kv_lens, void *hip_stream);
 
+/* ---- causal layers: gated delta rule -------------------------------------------------------------
+ * The recurrent, causal counterpart of the layer's linear branch: a state S [d, d] per head (key channel, value channel) that
+ * forgets by a gate and writes by the delta rule,
+ *   u_t = beta_t (v_t - e^g_t S_{t-1}^T k_t),   S_t = e^g_t S_{t-1} + k_t u_t^T,   out_t = scale S_t^T q_t.
+ *   q, k [B,Hk,N,d], v, out [B,H,N,d], H a multiple of Hk: value head h reads query and key head h / (H / Hk).  d is 64 or 128.
+ *   g, beta    fp32 [B,H,N]: logarithm of the decay (0 keeps, -infinity forgets all) and writing strength.  The state stays bounded
+ *              where |k| <= 1, 0 <= beta <= 2 and g <= 0; that and the normalisation of q and k are the caller's.
+ *   states     fp32 [B,H,d,d].  state_in NULL: zeros.  state_out NULL: not wanted; it may be state_in itself (in place).
+ *   lens       device int32 [B] or NULL (= N): tokens of each sample of a padded batch.  What lies behind is not read and left as it was;
+ *              a sample without tokens hands its state on.  Values outside 0..N are taken as the nearer end.
+ * Up to 32 tokens go one after the other with the state in registers; more go in chunks of 64 on the matrix cores.  The
+ * two agree up to rounding.  Everything in the chain of states is fp32, or split so that it keeps fp32's bits.  No atomics: the same bits for
+ * the same call. */
+typedef struct salad_delta_params {
+    int32_t B, H, Hk, N, d;
+    int32_t dtype;              /* salad_dtype of q, k, v, out and their gradients                  */
+    float scale;                /* 0 selects 1/sqrt(d)                                              */
+    const void *q, *k, *v;      /* device, 16-byte aligned like every tensor here                   */
+    const float *g, *beta;
+    void *out;                  /* forward only                                                     */
+    const float *state_in;
+    float *state_out;           /* forward only                                                     */
+    const int32_t *lens;
+    const void *dout;           /* backward only: [B,H,N,d]                                         */
+    const float *dstate_out;    /* backward only: gradient of the last state; NULL: zeros           */
+    void *dq, *dk, *dv;         /* backward only, shapes of q, k, v                                 */
+    float *dg, *dbeta;          /* backward only, [B,H,N]                                           */
+    float *dstate_in;           /* backward only: gradient of state_in; NULL: not wanted            */
+    void *workspace;            /* device, 256-byte aligned, salad_gated_delta_workspace_bytes(); NULL where that is 0 */
+    size_t workspace_bytes;
+    void *hip_stream;
+} salad_delta_params;
+
+/* Device scratch of a call (reads the shape and dtype only; 0 if none is needed or the shape is invalid).  Nothing in it has to be set or kept
+ * between calls, but calls that may overlap must not share one. */
+size_t salad_gated_delta_workspace_bytes(const salad_delta_params *p, int32_t backward);
+
+salad_status salad_gated_delta_fwd(const salad_delta_params *p);
+
+/* Gradients of sum(out * dout) + sum(state_out * dstate_out).  Takes the forward call's inputs and computes again what it needs. */
+salad_status salad_gated_delta_bwd(const salad_delta_params *p);
+
 /* ---- per-kernel timing ----------------------------------------------------------------------- */
 
 typedef struct salad_kernel_times {

@@ -16,7 +16,7 @@ _CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libsalad.so")
 SOURCES = ["salad_api.hip", "mask_gate_finalize.hip", "linear_state.hip", "sparse_attn.hip", "sparse_attn_f32.hip",
            "sparse_attn_v2.hip", "sparse_attn_v5.hip", "linear_apply.hip", "proj.hip", "topk.hip",
-           "causal_api.hip", "window_attn.hip", "window_grad.hip"]
+           "causal_api.hip", "window_attn.hip", "window_grad.hip", "delta_step.hip", "delta_chunk.hip", "delta_grad.hip"]
 
 SALAD_OK, SALAD_EINVAL, SALAD_ENOTSUP, SALAD_ENOSPC, SALAD_EHIP = range(5)
 SALAD_F32, SALAD_BF16 = 0, 1
@@ -28,7 +28,8 @@ EXPORTS = ["salad_last_error", "salad_kept_from_sparsity", "salad_block_mask_nnz
            "salad_block_mask_nnz_mode", "salad_block_mask_mode",
            "salad_tile_lists_bytes", "salad_tile_lists", "salad_proj_pack_bytes", "salad_proj_pack", "salad_fwd_workspace_bytes", "salad_sparse_linear_attn_fwd", "salad_linear_state_fwd",
            "salad_gate_fwd", "salad_gate_fwd_static", "salad_timing_enable", "salad_timing_read", "salad_tune",
-           "salad_window_attn_workspace_bytes", "salad_window_attn_fwd", "salad_window_attn_bwd", "salad_window_cache_append"]
+           "salad_window_attn_workspace_bytes", "salad_window_attn_fwd", "salad_window_attn_bwd", "salad_window_cache_append",
+           "salad_gated_delta_workspace_bytes", "salad_gated_delta_fwd", "salad_gated_delta_bwd"]
 
 
 class SaladError(RuntimeError):
@@ -80,6 +81,12 @@ class WindowParams(C.Structure):
         ("softmax_scale", C.c_float)] + [
         (n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "q_lens", "kv_lens", "dout", "dq", "dk", "dv", "workspace")] + [
         ("workspace_bytes", C.c_size_t), ("hip_stream", C.c_void_p)]
+
+
+class DeltaParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "H", "Hk", "N", "d", "dtype")] + [("scale", C.c_float)] + [
+        (n, C.c_void_p) for n in ("q", "k", "v", "g", "beta", "out", "state_in", "state_out", "lens", "dout", "dstate_out", "dq", "dk", "dv",
+                                  "dg", "dbeta", "dstate_in", "workspace")] + [("workspace_bytes", C.c_size_t), ("hip_stream", C.c_void_p)]
 
 
 class KernelTimes(C.Structure):
@@ -172,6 +179,10 @@ def lib() -> C.CDLL:
             f.restype, f.argtypes = C.c_int, [C.POINTER(WindowParams)]
         L.salad_window_cache_append.restype = C.c_int
         L.salad_window_cache_append.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 8 + [C.c_void_p] * 3
+        L.salad_gated_delta_workspace_bytes.restype = C.c_size_t
+        L.salad_gated_delta_workspace_bytes.argtypes = [C.POINTER(DeltaParams), C.c_int32]
+        for f in (L.salad_gated_delta_fwd, L.salad_gated_delta_bwd):
+            f.restype, f.argtypes = C.c_int, [C.POINTER(DeltaParams)]
         L.salad_tune.restype = C.c_int
         L.salad_tune.argtypes = [C.c_char_p, C.c_int32]
         _lib = L
@@ -426,7 +437,7 @@ def salad_tune(key: str, value: int) -> None:
 
 
 # ---------------------------------------------------------------------------------------------
-# causal layers: window attention with sinks
+# causal layers: window attention with sinks, gated delta rule
 # ---------------------------------------------------------------------------------------------
 
 class CausalWorkspace:
@@ -574,3 +585,65 @@ def salad_window_cache_append(k_new, v_new, k_cache, v_cache, sinks: int, kv_len
             _tensor("k_cache", k_cache, (B, Hk, Nk, d), dt, dev), _tensor("v_cache", v_cache, (B, Hk, Nk, d), dt, dev)]
     lens = [_tensor("q_lens", q_lens, (B,), torch.int32, dev, optional=True), _tensor("kv_lens", kv_lens, (B,), torch.int32, dev)]
     _call_on(dev, lambda: _check(lib().salad_window_cache_append(*ptrs, B, Hk, Nq, Nk, d, code, int(sinks), int(bool(ring)), *lens, _stream())))
+
+
+def _delta_params(q, k, v, g, beta, state, lens, scale):
+    import torch
+    p = DeltaParams()
+    p.dtype = _query(q)
+    B, Hk, N, d = q.shape
+    if v.dim() != 4:
+        raise ValueError(f"v has {v.dim()} dimensions, expected [B, H, N, d]")
+    H, dev = v.shape[1], q.device
+    p.B, p.H, p.Hk, p.N, p.d, p.scale = B, H, Hk, N, d, scale
+    p.q = _tensor("q", q, q.shape, q.dtype, dev)
+    p.k = _tensor("k", k, q.shape, q.dtype, dev)
+    p.v = _tensor("v", v, (B, H, N, d), q.dtype, dev)
+    p.g = _tensor("g", g, (B, H, N), torch.float32, dev)
+    p.beta = _tensor("beta", beta, (B, H, N), torch.float32, dev)
+    p.state_in = _tensor("state", state, (B, H, d, d), torch.float32, dev, optional=True)
+    p.lens = _tensor("lens", lens, (B,), torch.int32, dev, optional=True)
+    return p
+
+
+def salad_gated_delta_fwd(q, k, v, g, beta, *, state=None, state_out=None, lens=None, scale: float = 0.0, out=None,
+                          workspace: Optional[CausalWorkspace] = None):
+    """The gated delta rule over the tokens of a call, any number: q, k [B,Hk,N,d], v [B,H,N,d], g and beta fp32 [B,H,N] and a
+    state fp32 [B,H,d,d] (None: zeros) -> (out [B,H,N,d], the state after the last token).  `state_out` may be `state` itself."""
+    import torch
+    p = _delta_params(q, k, v, g, beta, state, lens, scale)
+
+    def call():
+        o = torch.empty_like(v) if out is None else out
+        s = torch.empty(p.B, p.H, p.d, p.d, dtype=torch.float32, device=q.device) if state_out is None else state_out
+        p.out = _tensor("out", o, v.shape, q.dtype, q.device)
+        p.state_out = _tensor("state_out", s, (p.B, p.H, p.d, p.d), torch.float32, q.device)
+        keep = _with_workspace(p, int(lib().salad_gated_delta_workspace_bytes(C.byref(p), 0)), workspace, q.device)
+        _check(lib().salad_gated_delta_fwd(C.byref(p)))
+        del keep
+        return o, s
+    return _call_on(q.device, call)
+
+
+def salad_gated_delta_bwd(q, k, v, g, beta, dout, *, state=None, dstate_out=None, lens=None, scale: float = 0.0, dq=None, dk=None, dv=None,
+                          dg=None, dbeta=None, dstate=None, workspace: Optional[CausalWorkspace] = None):
+    """Gradients (dq, dk, dv, dg, dbeta, dstate) of sum(out * dout) + sum(state_out * dstate_out) for salad_gated_delta_fwd with the same
+    inputs; dstate is the gradient of the state before the first token."""
+    import torch
+    p = _delta_params(q, k, v, g, beta, state, lens, scale)
+
+    def call():
+        p.dout = _tensor("dout", dout, v.shape, q.dtype, q.device)
+        p.dstate_out = _tensor("dstate_out", dstate_out, (p.B, p.H, p.d, p.d), torch.float32, q.device, optional=True)
+        grads = []
+        for n, given, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v), ("dg", dg, g), ("dbeta", dbeta, beta)):
+            x = torch.empty_like(like) if given is None else given
+            setattr(p, n, _tensor(n, x, like.shape, like.dtype, q.device))
+            grads.append(x)
+        s = torch.empty(p.B, p.H, p.d, p.d, dtype=torch.float32, device=q.device) if dstate is None else dstate
+        p.dstate_in = _tensor("dstate", s, (p.B, p.H, p.d, p.d), torch.float32, q.device)
+        keep = _with_workspace(p, int(lib().salad_gated_delta_workspace_bytes(C.byref(p), 1)), workspace, q.device)
+        _check(lib().salad_gated_delta_bwd(C.byref(p)))
+        del keep
+        return (*grads, s)
+    return _call_on(q.device, call)

@@ -91,16 +91,20 @@ struct DeltaArgs {
     int B, H, Hk, N, D, bf16;
     float scale;
     int chunks;                     // of 64 tokens
-    // workspace
-    u16 *tf;                        // [BH][chunks]: T = (I + A)^-1 in three bf16 planes, fragment order
-    void *s0;                       // [BH][chunks][D][D] the state before each chunk, transposed (value channel, key channel)
-    void *u;                        // [BH][chunks][D][64] u of each chunk, transposed
+    // workspace, by (sample, head, chunk of 64 tokens)
+    u16 *tf, *ttf;                  // T = (I + A)^-1 and (backward) its transpose: three bf16 planes in operand order
+    struct DeltaGate *gate;         // [64] each
+    float2 *bsum;                   // [64] each: running sum of g as two floats
+    void *s0;                       // [D][D] the state before the chunk, transposed (value channel, key channel); forward: the tensors' type, backward: fp32
+    void *u;                        // [D][64] u, transposed; likewise
     // backward
     const void *dout;
     const float *dstate_out;
     void *dq, *dk, *dv;
     float *dg, *dbeta, *dstate_in;
-    float *ds1, *du;                // gradients of the state behind each chunk and of u, laid out like s0 and u
+    float *ds1;                     // [D][D] gradient of the state behind the chunk, transposed
+    float *dr;                      // [D][64] first X = P^T dout, then dR = T^T du, transposed
+    float *dbv;                     // [D/16][64] sums of dR v over 16 value channels
     float *dq_part, *dk_part;       // [B,H,N,D] where heads share queries and keys, else null
 };
 __host__ __device__ inline int delta_len(const DeltaArgs &a, int b)
@@ -108,7 +112,11 @@ __host__ __device__ inline int delta_len(const DeltaArgs &a, int b)
     const int n = a.lens ? a.lens[b] : a.N;
     return n < 0 ? 0 : n > a.N ? a.N : n;
 }
+bool delta_takes_step(const DeltaArgs &a);
 hipError_t launch_delta_step(const DeltaArgs &a, hipStream_t st);
+// steps shared by both directions
+hipError_t launch_delta_chunk(const DeltaArgs &a, hipStream_t st);
+hipError_t launch_delta_scan(const DeltaArgs &a, bool backward, hipStream_t st);
 hipError_t launch_delta_fwd(const DeltaArgs &a, hipStream_t st);
 hipError_t launch_delta_bwd(const DeltaArgs &a, hipStream_t st);
 

@@ -4,8 +4,10 @@
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
+#include <type_traits>
 
 #include "causal.h"
+#include "delta_planes.h"
 #include "salad_status.h"
 
 using namespace salad;
@@ -99,9 +101,113 @@ WindowWs window_ws(WindowArgs &a, int dtype, bool backward)
     return w;
 }
 
+// ---- gated delta rule -----------------------------------------------------------------------------
+salad_status delta_shape(const char *who, const salad_delta_params *p)
+{
+    if (p->dtype != SALAD_BF16 && p->dtype != SALAD_F32) return fail(SALAD_EINVAL, "%s: dtype %d", who, (int)p->dtype);
+    if (p->d != 64 && p->d != 128) return fail(SALAD_ENOTSUP, "%s: d=%d (64 or 128)", who, (int)p->d);
+    if (p->B < 1 || p->H < 1 || p->Hk < 1 || p->N < 1)
+        return fail(SALAD_EINVAL, "%s: B=%d H=%d Hk=%d N=%d must be positive", who, (int)p->B, (int)p->H, (int)p->Hk, (int)p->N);
+    if (p->H % p->Hk) return fail(SALAD_EINVAL, "%s: H=%d is not a multiple of Hk=%d", who, (int)p->H, (int)p->Hk);
+    if (!std::isfinite(p->scale)) return fail(SALAD_EINVAL, "%s: scale is not finite", who);
+    // workgroups (two a chunk of 64 tokens, eight a head) are counted in 32 bits
+    if ((double)p->B * p->H * (((double)p->N + 63) / 64 * 2 + 8) > 16e6 || (double)p->B * p->Hk * p->N * p->d / 4 > 4e9)
+        return fail(SALAD_ENOTSUP, "%s: B*H*N too large for one launch", who);
+    return SALAD_OK;
+}
+
+DeltaArgs delta_args(const salad_delta_params *p)
+{
+    DeltaArgs a{};
+    a.q = p->q; a.k = p->k; a.v = p->v; a.g = p->g; a.beta = p->beta;
+    a.out = p->out; a.state_in = p->state_in; a.state_out = p->state_out; a.lens = p->lens;
+    a.B = p->B; a.H = p->H; a.Hk = p->Hk; a.N = p->N; a.D = p->d;
+    a.bf16 = p->dtype == SALAD_BF16;
+    a.scale = p->scale == 0.f ? 1.f / std::sqrt((float)p->d) : p->scale;
+    a.chunks = (p->N + DELTA_C - 1) / DELTA_C;
+    a.dout = p->dout; a.dstate_out = p->dstate_out;
+    a.dq = p->dq; a.dk = p->dk; a.dv = p->dv; a.dg = p->dg; a.dbeta = p->dbeta; a.dstate_in = p->dstate_in;
+    return a;
+}
+
+// Lays the scratch out from `ws` on (null: only counts); returns the bytes.
+size_t delta_ws(DeltaArgs &a, bool backward, char *ws)
+{
+    if (!backward && delta_takes_step(a)) return 0;
+    const size_t BH = (size_t)a.B * a.H, n = BH * a.chunks, es = a.bf16 && !backward ? sizeof(u16) : sizeof(float), D = a.D;
+    size_t off = 0;
+    auto take = [&](auto *&to, size_t bytes) { to = (std::remove_reference_t<decltype(to)>)(ws + off); off = align256(off + bytes); };
+    take(a.tf, n * DELTA_T_ELEMS * sizeof(u16));
+    take(a.gate, n * 64 * sizeof(DeltaGate));
+    take(a.bsum, n * 64 * sizeof(float2));
+    take(a.s0, n * D * D * es);
+    take(a.u, n * D * 64 * es);
+    if (backward) {
+        take(a.ttf, n * DELTA_T_ELEMS * sizeof(u16));
+        take(a.ds1, n * D * D * sizeof(float));
+        take(a.dr, n * D * 64 * sizeof(float));
+        take(a.dbv, n * D / 16 * 64 * sizeof(float));
+        if (a.H != a.Hk) {
+            take(a.dq_part, BH * a.N * D * sizeof(float));
+            take(a.dk_part, BH * a.N * D * sizeof(float));
+        }
+    }
+    return off;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t salad_gated_delta_workspace_bytes(const salad_delta_params *p, int32_t backward)
+{
+    if (!p || delta_shape("salad_gated_delta_workspace_bytes", p) != SALAD_OK) return 0;
+    DeltaArgs a = delta_args(p);
+    return delta_ws(a, backward != 0, nullptr);
+}
+
+salad_status salad_gated_delta_fwd(const salad_delta_params *p)
+{
+    const char *who = "salad_gated_delta_fwd";
+    if (!p) return fail(SALAD_EINVAL, "%s: null params", who);
+    if (const salad_status s = delta_shape(who, p)) return s;
+    if (!p->q || !p->k || !p->v || !p->g || !p->beta || !p->out) return fail(SALAD_EINVAL, "%s: null pointer", who);
+    for (const void *x : {p->q, p->k, p->v, (const void *)p->g, (const void *)p->beta, (const void *)p->state_in})
+        if (p->out == x || (p->state_out && x != p->state_in && p->state_out == x)) return fail(SALAD_EINVAL, "%s: an output aliases an input", who);
+    if (p->out == p->state_out) return fail(SALAD_EINVAL, "%s: out and state_out share a buffer", who);
+    if (!aligned16({p->q, p->k, p->v, p->out, p->state_in, p->state_out})) return fail(SALAD_EINVAL, "%s: a tensor is not 16-byte aligned", who);
+    DeltaArgs a = delta_args(p);
+    if (const salad_status s = check_workspace(who, p->workspace, p->workspace_bytes, delta_ws(a, false, nullptr))) return s;
+    delta_ws(a, false, (char *)p->workspace);
+    const hipStream_t st = (hipStream_t)p->hip_stream;
+    const hipError_t e = delta_takes_step(a) ? launch_delta_step(a, st) : launch_delta_fwd(a, st);
+    return e == hipSuccess ? SALAD_OK : hip_fail(e, who);
+}
+
+salad_status salad_gated_delta_bwd(const salad_delta_params *p)
+{
+    const char *who = "salad_gated_delta_bwd";
+    if (!p) return fail(SALAD_EINVAL, "%s: null params", who);
+    if (const salad_status s = delta_shape(who, p)) return s;
+    if (!p->q || !p->k || !p->v || !p->g || !p->beta || !p->dout || !p->dq || !p->dk || !p->dv || !p->dg || !p->dbeta)
+        return fail(SALAD_EINVAL, "%s: null pointer", who);
+    const void *grads[] = {p->dq, p->dk, p->dv, p->dg, p->dbeta, p->dstate_in};
+    for (int i = 0; i < 6; ++i) {
+        if (!grads[i]) continue;
+        for (const void *x : {p->q, p->k, p->v, (const void *)p->g, (const void *)p->beta, (const void *)p->state_in, p->dout, (const void *)p->dstate_out})
+            if (grads[i] == x) return fail(SALAD_EINVAL, "%s: a gradient aliases an input", who);
+        for (int j = 0; j < i; ++j)
+            if (grads[i] == grads[j]) return fail(SALAD_EINVAL, "%s: two gradients share a buffer", who);
+    }
+    if (!aligned16({p->q, p->k, p->v, p->dout, p->dq, p->dk, p->dv, p->state_in, p->dstate_out, p->dstate_in}))
+        return fail(SALAD_EINVAL, "%s: a tensor is not 16-byte aligned", who);
+    DeltaArgs a = delta_args(p);
+    if (const salad_status s = check_workspace(who, p->workspace, p->workspace_bytes, delta_ws(a, true, nullptr))) return s;
+    delta_ws(a, true, (char *)p->workspace);
+    a.state_out = nullptr;
+    const hipError_t e = launch_delta_bwd(a, (hipStream_t)p->hip_stream);
+    return e == hipSuccess ? SALAD_OK : hip_fail(e, who);
+}
 
 size_t salad_window_attn_workspace_bytes(const salad_window_params *p, int32_t backward)
 {

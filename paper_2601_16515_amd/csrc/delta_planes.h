@@ -1,0 +1,163 @@
+// Products of the delta rule's kernels: v_mfma_f32_16x16x32_bf16 on operands kept as one or three bf16 planes.
+//
+// The state, u and their gradients are fp32 results of long recurrences, and their products have to keep that.  A float x is
+// x0 + x1 + x2 with x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1): 24 bits, exact but for values below the range.  The product
+// of three planes by three takes the six terms down to 2^-16 of the first (what is left out is below 2^-24), by a tensor that is bf16
+// already three.  The fp32 matrix instruction has a sixteenth of the bf16 rate: six products are 2.7 times faster, three 5.3 times.
+//
+// Lane l of an operand holds row l % 16 and the 8 contraction indices from 8 (l / 16) on; accumulator r is row 4 (l / 16) + r,
+// column l % 16.  An LDS tile is row-major with `pitch` elements a row; it serves as an operand along its rows (frag_n) or, by
+// transposing reads, along its columns (frag_t).
+#pragma once
+#include "causal.h"
+
+namespace salad {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace {
+
+#define LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+
+__device__ inline uint32_t pack2(float a, float b)
+{
+    f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+__device__ inline float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+template <int P> struct Op { bf16x8 p[P]; };
+
+// c += A B, the small terms first
+template <int PA, int PB>
+__device__ inline void mma(f32x4 &c, const Op<PA> &a, const Op<PB> &b)
+{
+#pragma unroll
+    for (int s = 2; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (s - i >= 0 && s - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
+}
+
+// four floats as P planes
+template <int P>
+__device__ inline void split4(f32x4 x, u32x2 (&o)[P])
+{
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        o[p].x = pack2(x[0], x[1]);
+        o[p].y = pack2(x[2], x[3]);
+        if (p + 1 < P) x -= f32x4{low(o[p].x), high(o[p].x), low(o[p].y), high(o[p].y)};
+    }
+}
+// 4 floats into 4 neighbouring elements of a tile's planes
+template <int P>
+__device__ inline void put4(u16 *tile, int plane, f32x4 x)
+{
+    u32x2 o[P];
+    split4<P>(x, o);
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<u32x2 *>(tile + p * plane) = o[p];
+}
+
+// operand whose row is row r0 + l % 16 of the tile, contraction along the row from k0 on
+template <int P>
+__device__ inline Op<P> frag_n(const u16 *tile, int plane, int pitch, int r0, int k0, int lane)
+{
+    Op<P> f;
+    const u16 *at = tile + (r0 + (lane & 15)) * pitch + k0 + 8 * (lane >> 4);
+#pragma unroll
+    for (int p = 0; p < P; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(at + p * plane);
+    return f;
+}
+// operand whose row is column c0 + l % 16 of the tile, contraction down the column from row k0 on.  Each group of 16 lanes
+// transposes 4 rows x 16 columns; the lane supplies the address of row (l / 4) % 4, columns 4 (l % 4) on.
+template <int P>
+__device__ inline Op<P> frag_t(const u16 *tile, int plane, int pitch, int c0, int k0, int lane)
+{
+    union { bf16x8 v; s16x4 h[2]; } u;
+    Op<P> f;
+    const u16 *at = tile + (k0 + 8 * (lane >> 4) + ((lane >> 2) & 3)) * pitch + c0 + 4 * (lane & 3);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane + 4 * pitch));
+        f.p[p] = u.v;
+    }
+    return f;
+}
+
+// a tensor's type: planes of its operands, 4 neighbouring values as floats
+template <typename T> constexpr int planes_of() { return sizeof(T) == 2 ? 1 : 3; }
+__device__ inline f32x4 load4(const u16 *p)
+{
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    return f32x4{low(w.x), high(w.x), low(w.y), high(w.y)};
+}
+__device__ inline f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+__device__ inline float load1(const u16 *p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ inline float load1(const float *p) { return *p; }
+__device__ inline void store1(u16 *p, float x) { *p = (u16)pack2(x, 0.f); }
+__device__ inline void store1(float *p, float x) { *p = x; }
+__device__ inline void store4(u16 *p, f32x4 x) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
+__device__ inline void store4(float *p, f32x4 x) { *reinterpret_cast<f32x4 *>(p) = x; }
+
+// operand straight from a tensor's row (zeros where !ok): 8 values from p on
+__device__ inline Op<1> frag_g(const u16 *p, bool ok)
+{
+    u32x4 w = {0, 0, 0, 0};
+    if (ok) w = *reinterpret_cast<const u32x4 *>(p);
+    return Op<1>{{__builtin_bit_cast(bf16x8, w)}};
+}
+__device__ inline Op<3> frag_g(const float *p, bool ok)
+{
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    if (ok) { x = *reinterpret_cast<const f32x4 *>(p); y = *reinterpret_cast<const f32x4 *>(p + 4); }
+    u32x2 a[3], b[3];
+    split4<3>(x, a);
+    split4<3>(y, b);
+    Op<3> f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) f.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[i].x, a[i].y, b[i].x, b[i].y});
+    return f;
+}
+
+// 64 rows x D of a tensor on their way to an LDS tile: 256 threads load them into registers, and put them down later
+template <typename T, int D> struct Tile64 {
+    static constexpr int P = planes_of<T>(), PITCH = D + 8, PLANE = 64 * PITCH, PER = 16 / sizeof(T), LPR = D / PER, RPP = 256 / LPR, NP = 64 / RPP;
+    u32x4 r[NP];
+    __device__ inline void load(const T *base, int valid, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int row = i * RPP + tid / LPR;
+            r[i] = u32x4{0, 0, 0, 0};
+            if (row < valid) r[i] = *reinterpret_cast<const u32x4 *>(base + (size_t)row * D + tid % LPR * PER);
+        }
+    }
+    __device__ inline void store(u16 *tile, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            u16 *at = tile + (i * RPP + tid / LPR) * PITCH + tid % LPR * PER;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x4 *>(at) = r[i];
+            else put4<3>(at, PLANE, __builtin_bit_cast(f32x4, r[i]));
+        }
+    }
+};
+
+}  // namespace
+
+// per token of a chunk, for the kernels behind delta_chunk_kernel (zeros for tokens that are not there)
+struct DeltaGate { float gamma, tail, beta, pad; };     // exp(b_i), exp(b_63 - b_i), beta_i with b the running sum of g
+constexpr int DELTA_C = 64;
+constexpr size_t DELTA_T_ELEMS = 3 * 4 * 2 * 64 * 8;    // T of a chunk: planes, row tiles, halves of the contraction, lanes, 8 each
+
+}  // namespace salad

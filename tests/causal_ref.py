@@ -72,3 +72,39 @@ def window_gradients(q, k, v, out, lse, dout, window, sinks, q_lens=None, kv_len
                 c[t][b, at, :n] += f * (m.abs() @ w.abs())
                 e[t][b, at, :n] += f * (em @ w.abs())
     return g, c, e
+
+
+def gated_delta(q, k, v, g, beta, state=None, lens=None, scale=None):
+    """out, last state, and scale |q| M with M the state's terms summed by magnitude (what roundings of its factors cost): token by
+    token, differentiable.  lens: list."""
+    B, Hk, N, d = q.shape
+    H = v.shape[1]
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    q, k = (x.to(F64).repeat_interleave(H // Hk, 1) for x in (q, k))
+    v, g, beta = v.to(F64), g.to(F64), beta.to(F64)
+    S = torch.zeros(B, H, d, d, dtype=F64, device=q.device) if state is None else state.to(F64)
+    M, outs, costs = S.abs().detach(), [], []
+    for t in range(N):
+        live = torch.tensor([lens is None or t < n for n in (lens or [N] * B)], device=q.device)[:, None, None, None]
+        kt, qt, a = (torch.where(live[..., 0], x[:, :, t], 0.0) for x in (k, q, g[..., None].exp()))
+        S1 = a[..., None] * S
+        u = beta[:, :, t, None] * (v[:, :, t] - (kt[:, :, None] @ S1)[:, :, 0])
+        u = torch.where(live[..., 0], u, 0.0)
+        S = torch.where(live, S1 + kt[..., None] * u[:, :, None], S)
+        M = torch.where(live, a[..., None] * M + (kt[..., None] * u[:, :, None]).abs(), M).detach()
+        outs.append(scale * (qt[:, :, None] @ S)[:, :, 0])
+        costs.append(scale * (qt.abs()[:, :, None] @ M)[:, :, 0].detach())
+    return torch.stack(outs, 2), S, torch.stack(costs, 2)
+
+
+def gated_delta_gradients(q, k, v, g, beta, dout, state=None, dstate_out=None, lens=None, scale=None):
+    """(dq, dk, dv, dg, dbeta, dstate) by differentiation of the above."""
+    B, H, d = v.shape[0], v.shape[1], v.shape[3]
+    S = torch.zeros(B, H, d, d, dtype=F64, device=q.device) if state is None else state
+    x = [t.to(F64).clone().requires_grad_() for t in (q, k, v, g, beta, S)]
+    out, last, _ = gated_delta(*x, lens, scale)
+    live = torch.tensor([[t < n for t in range(v.shape[2])] for n in (lens or [v.shape[2]] * B)], device=q.device)[:, None, :, None]
+    loss = (out * torch.where(live, dout.to(F64), 0.0)).sum()
+    if dstate_out is not None:
+        loss = loss + (last * dstate_out.to(F64)).sum()
+    return torch.autograd.grad(loss, x)
