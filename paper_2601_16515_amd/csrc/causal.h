@@ -93,10 +93,12 @@ struct DeltaArgs {
     int chunks;                     // of 64 tokens
     // workspace, by (sample, head, chunk of 64 tokens)
     u16 *tf, *ttf;                  // T = (I + A)^-1 and (backward) its transpose: three bf16 planes in operand order
-    struct DeltaGate *gate;         // [64] each
+    struct DeltaGate *gate;
     float2 *bsum;                   // [64] each: running sum of g as two floats
-    void *s0;                       // [D][D] the state before the chunk, transposed (value channel, key channel); forward: the tensors' type, backward: fp32
-    void *u;                        // [D][64] u, transposed; likewise
+    u16 *pf;                        // forward: P in operand order, one plane for bf16 tensors, three for fp32
+    // backward: what the gradients need of the forward pass
+    float *s0;                      // [D][D] the state before the chunk, transposed (value channel, key channel)
+    float *u;                       // [D][64] u, transposed
     // backward
     const void *dout;
     const float *dstate_out;
@@ -116,7 +118,7 @@ bool delta_takes_step(const DeltaArgs &a);
 hipError_t launch_delta_step(const DeltaArgs &a, hipStream_t st);
 // steps shared by both directions
 hipError_t launch_delta_chunk(const DeltaArgs &a, hipStream_t st);
-hipError_t launch_delta_scan(const DeltaArgs &a, bool backward, hipStream_t st);
+hipError_t launch_delta_chains(const DeltaArgs &a, bool backward, hipStream_t st);
 hipError_t launch_delta_fwd(const DeltaArgs &a, hipStream_t st);
 hipError_t launch_delta_bwd(const DeltaArgs &a, hipStream_t st);
 

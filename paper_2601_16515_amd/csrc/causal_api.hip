@@ -134,15 +134,17 @@ DeltaArgs delta_args(const salad_delta_params *p)
 size_t delta_ws(DeltaArgs &a, bool backward, char *ws)
 {
     if (!backward && delta_takes_step(a)) return 0;
-    const size_t BH = (size_t)a.B * a.H, n = BH * a.chunks, es = a.bf16 && !backward ? sizeof(u16) : sizeof(float), D = a.D;
+    const size_t BH = (size_t)a.B * a.H, n = BH * a.chunks, D = a.D;
     size_t off = 0;
     auto take = [&](auto *&to, size_t bytes) { to = (std::remove_reference_t<decltype(to)>)(ws + off); off = align256(off + bytes); };
     take(a.tf, n * DELTA_T_ELEMS * sizeof(u16));
-    take(a.gate, n * 64 * sizeof(DeltaGate));
+    take(a.gate, n * sizeof(DeltaGate));
     take(a.bsum, n * 64 * sizeof(float2));
-    take(a.s0, n * D * D * es);
-    take(a.u, n * D * 64 * es);
-    if (backward) {
+    if (!backward) {
+        take(a.pf, n * (a.bf16 ? 1 : 3) * 4 * 2 * 64 * 8 * sizeof(u16));
+    } else {
+        take(a.s0, n * D * D * sizeof(float));
+        take(a.u, n * D * 64 * sizeof(float));
         take(a.ttf, n * DELTA_T_ELEMS * sizeof(u16));
         take(a.ds1, n * D * D * sizeof(float));
         take(a.dr, n * D * 64 * sizeof(float));

@@ -2,7 +2,7 @@
 // the states before the chunks and U are computed again.  With dS the gradient of the state behind a chunk,
 //   dU = X + tail K dS,   X = P^T dO,          dR = T^T dU,
 //   gradient of the state before the chunk = gamma_63 dS + Q^T (scale gamma dO) - K^T (beta gamma dR),
-// a chain from the last chunk to the first like the forward one, and then for every chunk at once, with dA = -(dR U^T) below the diagonal
+// a chain from the last chunk to the first like the forward one (delta_chain.hip), and then for every chunk at once, with dA = -(dR U^T) below the diagonal
 // and dP = dO U^T,
 //   dv = beta dR,
 //   dq = scale gamma dO S_0^T + (scale e^(b_i - b_j) dP) K,
@@ -39,13 +39,13 @@ __global__ __launch_bounds__(256) void delta_x_kernel(DeltaArgs a)
     const float2 bi = a.bsum[at * 64 + tok];
     Op<P> k[NK];
 #pragma unroll
-    for (int x = 0; x < NK; ++x) k[x] = frag_g(kp + (size_t)tok * D + x * 32 + 8 * l4, tok < valid);
+    for (int x = 0; x < NK; ++x) k[x] = frag_g(kp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, tok < valid);
 #pragma unroll
     for (int it = 0; it < 4; ++it) {
         f32x4 c = {0.f, 0.f, 0.f, 0.f};
         if (it >= wave) {
 #pragma unroll
-            for (int x = 0; x < NK; ++x) mma(c, frag_g(qp + (size_t)(16 * it + l16) * D + x * 32 + 8 * l4, 16 * it + l16 < valid), k[x]);
+            for (int x = 0; x < NK; ++x) mma(c, frag_g(qp + (size_t)min(16 * it + l16, valid - 1) * D + x * 32 + 8 * l4, 16 * it + l16 < valid), k[x]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = 16 * it + 4 * l4 + r;
@@ -66,116 +66,6 @@ __global__ __launch_bounds__(256) void delta_x_kernel(DeltaArgs a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[(16 * ct + 4 * l4 + r) * 64 + tok] = c[r];
     }
-}
-
-// ---- gradients of the states, from the last chunk to the first ---------------------------------------------
-// Like delta_scan_kernel; also dv, and the sums of dR v that dbeta takes.
-template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void delta_scan_grad_kernel(DeltaArgs a)
-{
-    constexpr int P = planes_of<T>(), NT = D / 64, NK = D / 32, SP = D + 8, UP = 72;
-    using Tile = Tile64<T, D>;
-    extern __shared__ __attribute__((aligned(16))) u16 lds[];
-    u16 *Kt = lds, *Qt = Kt + P * Tile::PLANE, *St = Qt + P * Tile::PLANE, *Ut = St + 3 * 16 * SP, *Wt = Ut + 3 * 16 * UP, *Gt = Wt + 3 * 16 * UP;
-    const int slices = D / 16;
-    const int bh = blockIdx.x / slices, slice = blockIdx.x - bh * slices, c0 = slice * 16, b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, l4 = lane >> 4;
-    const int len = delta_len(a, b), chunks = (len + 63) / 64;
-    const T *kp = reinterpret_cast<const T *>(a.k) + ((size_t)b * a.Hk + hk) * a.N * D;
-    const T *qp = reinterpret_cast<const T *>(a.q) + ((size_t)b * a.Hk + hk) * a.N * D;
-    const T *vp = reinterpret_cast<const T *>(a.v) + (size_t)bh * a.N * D + c0 + l16;
-    const T *gp = reinterpret_cast<const T *>(a.dout) + (size_t)bh * a.N * D + c0 + l16;
-    T *dvp = reinterpret_cast<T *>(a.dv) + (size_t)bh * a.N * D + c0 + l16;
-    const int arow = wave * (D / 4) + 4 * l4;
-    f32x4 s[NT];
-#pragma unroll
-    for (int x = 0; x < NT; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[x][r] = a.dstate_out ? a.dstate_out[((size_t)bh * D + arow + 16 * x + r) * D + c0 + l16] : 0.f;
-    const int i0 = 16 * wave + 4 * l4;
-    Tile kr, qr;
-    Op<3> tn[2];
-    float vn[4], don[4];
-    f32x4 gn[4], xn;
-    float endn = 0.f;
-    auto fetch = [&](int ch) {
-        const size_t at = (size_t)bh * a.chunks + ch;
-        kr.load(kp + (size_t)ch * 64 * D, min(len - ch * 64, 64), tid);
-        qr.load(qp + (size_t)ch * 64 * D, min(len - ch * 64, 64), tid);
-        const u16 *tf = a.ttf + at * DELTA_T_ELEMS;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int p = 0; p < 3; ++p) tn[kt].p[p] = *reinterpret_cast<const bf16x8 *>(tf + (((p * 4 + wave) * 2 + kt) * 64 + lane) * 8);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const bool ok = ch * 64 + i0 + r < len;
-            vn[r] = ok ? load1(vp + (size_t)(ch * 64 + i0 + r) * D) : 0.f;
-            don[r] = ok ? load1(gp + (size_t)(ch * 64 + i0 + r) * D) : 0.f;
-            gn[r] = *reinterpret_cast<const f32x4 *>(a.gate + at * 64 + i0 + r);
-        }
-        xn = *reinterpret_cast<const f32x4 *>(a.dr + (at * D + c0 + l16) * 64 + i0);
-        endn = a.gate[at * 64 + 63].gamma;
-    };
-    if (chunks > 0) fetch(chunks - 1);
-    for (int ch = chunks - 1; ch >= 0; --ch) {
-        const size_t at = (size_t)bh * a.chunks + ch;
-        Op<3> tc[2] = {tn[0], tn[1]};
-        float vc[4];
-        f32x4 gc[4], x0 = xn, go;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { vc[r] = vn[r]; gc[r] = gn[r]; go[r] = a.scale * gn[r][0] * don[r]; }
-        const float end = endn;
-        kr.store(Kt, tid);
-        qr.store(Qt, tid);
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            put4<3>(St + l16 * SP + arow + 16 * x, 16 * SP, s[x]);
-            store4(a.ds1 + (at * D + c0 + l16) * D + arow + 16 * x, s[x]);
-        }
-        put4<3>(Gt + l16 * UP + i0, 16 * UP, go);
-        __syncthreads();
-        if (ch > 0) fetch(ch - 1);
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < NK; ++x) mma(acc, frag_n<P>(Kt, Tile::PLANE, Tile::PITCH, 16 * wave, 32 * x, lane), frag_n<3>(St, 16 * SP, SP, 0, 32 * x, lane));
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] = x0[r] + gc[r][1] * acc[r];
-        put4<3>(Ut + l16 * UP + i0, 16 * UP, acc);
-        __syncthreads();
-        f32x4 dr = {0.f, 0.f, 0.f, 0.f};
-        if (wave < 2) mma(dr, tc[0], frag_n<3>(Ut, 16 * UP, UP, 0, 0, lane));       // T^T is upper triangular
-        mma(dr, tc[1], frag_n<3>(Ut, 16 * UP, UP, 0, 32, lane));
-        store4(a.dr + (at * D + c0 + l16) * 64 + i0, dr);
-        f32x4 w;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float bd = gc[r][2] * dr[r];
-            if (ch * 64 + i0 + r < len) store1(dvp + (size_t)(ch * 64 + i0 + r) * D, bd);
-            w[r] = -gc[r][0] * bd;
-            float d = dr[r] * vc[r];                                    // over the 16 channels
-#pragma unroll
-            for (int m = 1; m < 16; m <<= 1) d += __shfl_xor(d, m);
-            if (l16 == 0) a.dbv[(at * slices + slice) * 64 + i0 + r] = d;
-        }
-        put4<3>(Wt + l16 * UP + i0, 16 * UP, w);
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            s[x] *= end;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                mma(s[x], frag_t<P>(Qt, Tile::PLANE, Tile::PITCH, wave * (D / 4) + 16 * x, 32 * kt, lane), frag_n<3>(Gt, 16 * UP, UP, 0, 32 * kt, lane));
-                mma(s[x], frag_t<P>(Kt, Tile::PLANE, Tile::PITCH, wave * (D / 4) + 16 * x, 32 * kt, lane), frag_n<3>(Wt, 16 * UP, UP, 0, 32 * kt, lane));
-            }
-        }
-        __syncthreads();                                                // K, Q and dO's tiles are written anew
-    }
-    if (a.dstate_in)
-#pragma unroll
-        for (int x = 0; x < NT; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) a.dstate_in[((size_t)bh * D + arow + 16 * x + r) * D + c0 + l16] = s[x][r];
 }
 
 // ---- the rest, every chunk at once ----------------------------------------------------------------------------
@@ -220,7 +110,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
             put4<3>(Rt + (i / 16) * UP + i % 16 * 4, UPL, load4(rp + i * 4));
         }
         __syncthreads();
-        const Op<P> go = frag_g(gp + (size_t)tok * D + cb * 32 + 8 * l4, live);
+        const Op<P> go = frag_g(gp + (size_t)min(tok, valid - 1) * D + cb * 32 + 8 * l4, live);
         const Op<3> ui = frag_t<3>(Ut, UPL, UP, 16 * wave, 0, lane), ri = frag_t<3>(Rt, UPL, UP, 16 * wave, 0, lane);
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
@@ -237,13 +127,13 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
                 mma(ou[x], uj, go);
             }
     }
-    const DeltaGate gt = a.gate[at * 64 + tok];
+    const float gamma = a.gate[at].gamma[tok], tail = a.gate[at].tail[tok], beta = a.gate[at].beta[tok];
     const float2 bi = a.bsum[at * 64 + tok];
     Op<P> ki[NK], qi[NK];
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
-        ki[x] = frag_g(kp + (size_t)tok * D + x * 32 + 8 * l4, live);
-        qi[x] = frag_g(qp + (size_t)tok * D + x * 32 + 8 * l4, live);
+        ki[x] = frag_g(kp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, live);
+        qi[x] = frag_g(qp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, live);
     }
     __syncthreads();                                                    // the blocks' tiles make room
     // pairs (i = own token, j): what A and P have to say
@@ -254,7 +144,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
         if (x <= wave) {
 #pragma unroll
             for (int y = 0; y < NK; ++y) {
-                const Op<P> kj = frag_g(kp + (size_t)(16 * x + l16) * D + y * 32 + 8 * l4, 16 * x + l16 < valid);
+                const Op<P> kj = frag_g(kp + (size_t)min(16 * x + l16, valid - 1) * D + y * 32 + 8 * l4, 16 * x + l16 < valid);
                 mma(kk, kj, ki[y]);
                 mma(qk, kj, qi[y]);
             }
@@ -264,7 +154,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
                 const float2 bj = a.bsum[at * 64 + j];
                 const float ratio = j <= tok ? expf((bi.x - bj.x) + (bi.y - bj.y)) : 0.f;
                 const float da = j < tok ? -ru[x][r] * ratio : 0.f;
-                e[r] = da * gt.beta;
+                e[r] = da * beta;
                 dp[r] = a.scale * ratio * ou[x][r];
                 cs[r] = j < tok ? e[r] * kk[r] + dp[r] * qk[r] : 0.f;   // by the decay between j and i; none from a token to itself
                 db += da * kk[r];
@@ -287,16 +177,16 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     for (int x = 0; x < NA; ++x) {
         f32x4 q4 = {0.f, 0.f, 0.f, 0.f}, k4 = q4;
         if (live) { q4 = load4(qp + (size_t)tok * D + 16 * x + 4 * l4); k4 = load4(kp + (size_t)tok * D + 16 * x + 4 * l4); }
-        qs[x] *= a.scale * gt.gamma;
-        ks[x] *= -gt.gamma;
-        ke[x] *= gt.tail;
+        qs[x] *= a.scale * gamma;
+        ks[x] *= -gamma;
+        ke[x] *= tail;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             db += ks[x][r] * k4[r];
-            rows += qs[x][r] * q4[r] + gt.beta * ks[x][r] * k4[r];
+            rows += qs[x][r] * q4[r] + beta * ks[x][r] * k4[r];
             end += ke[x][r] * k4[r];
         }
-        ks[x] = ks[x] * gt.beta + ke[x];
+        ks[x] = ks[x] * beta + ke[x];
     }
     rows -= end;
 #pragma unroll
@@ -305,7 +195,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     for (int m = 1; m < 16; m <<= 1) end += __shfl_xor(end, m);         // over the wave's tokens
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) sds += __shfl_xor(sds, m);
-    const float gend = a.gate[at * 64 + 63].gamma;
+    const float gend = a.gate[at].gamma[63];
     if (lane == 0) red[wave] = end + gend * sds;
     if (l4 == 0) {
         fin[tok] = rows;
@@ -390,15 +280,14 @@ template <typename T, int D>
 hipError_t run(const DeltaArgs &a, hipStream_t st)
 {
     constexpr int P = planes_of<T>(), tile = P * Tile64<T, D>::PLANE;
-    constexpr int x_bytes = (tile + 3 * 64 * 72) * 2, scan_bytes = (2 * tile + 3 * 16 * (D + 8) + 3 * 3 * 16 * 72) * 2;
+    constexpr int x_bytes = (tile + 3 * 64 * 72) * 2;
     constexpr int blocks = 2 * 3 * 32 * (D + 8) + 2 * 3 * 32 * 72, pairs = tile + 2 * P * 64 * 72, grad_bytes = (blocks > pairs ? blocks : pairs) * 2;
-    static bool dx[16], ds[16], dg[16];
+    static bool dx[16], dg[16];
     if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_x_kernel<T, D>), x_bytes, dx)) return e;
-    if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_scan_grad_kernel<T, D>), scan_bytes, ds)) return e;
     if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_grad_kernel<T, D>), grad_bytes, dg)) return e;
     const dim3 all(a.B * a.H * a.chunks);
     launch_kernel((delta_x_kernel<T, D>), all, dim3(256), x_bytes, st, a);
-    launch_kernel((delta_scan_grad_kernel<T, D>), dim3(a.B * a.H * (D / 16)), dim3(256), scan_bytes, st, a);
+    if (const hipError_t e = launch_delta_chains(a, true, st)) return e;
     launch_kernel((delta_grad_kernel<T, D>), all, dim3(256), grad_bytes, st, a);
     if (a.dq_part) {
         const long long total = (long long)a.B * a.Hk * a.N * D / 4;
@@ -412,7 +301,6 @@ hipError_t run(const DeltaArgs &a, hipStream_t st)
 hipError_t launch_delta_bwd(const DeltaArgs &a, hipStream_t st)
 {
     if (const hipError_t e = launch_delta_chunk(a, st)) return e;
-    if (const hipError_t e = launch_delta_scan(a, true, st)) return e;
     if (a.bf16) return a.D == 128 ? run<u16, 128>(a, st) : run<u16, 64>(a, st);
     return a.D == 128 ? run<float, 128>(a, st) : run<float, 64>(a, st);
 }

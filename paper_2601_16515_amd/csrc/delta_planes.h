@@ -33,6 +33,31 @@ __device__ inline uint32_t pack2(float a, float b)
 __device__ inline float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// A workgroup's barrier for what it exchanges through LDS.  __syncthreads() would also wait for every load and store to memory in flight, and
+// with that for the operands that are loaded a chunk ahead.
+__device__ inline void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A store that the hardware drops where `offset` is not below the size that the resource was made with.  Loads and stores are counted
+// together, in order: behind a store that may be skipped nobody could wait for an earlier load without waiting for the store, too.
+template <typename T>
+__device__ inline __amdgpu_buffer_rsrc_t bounded(T *p, int elems)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, elems * (int)sizeof(T), 0x00027000);
+}
+__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, u16, int elem, float x)
+{
+    __builtin_amdgcn_raw_buffer_store_b16((u16)pack2(x, 0.f), r, elem * 2, 0, 0);
+}
+__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, float, int elem, float x)
+{
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, elem * 4, 0, 0);
+}
+
 template <int P> struct Op { bf16x8 p[P]; };
 
 // c += A B, the small terms first
@@ -109,24 +134,28 @@ __device__ inline void store1(float *p, float x) { *p = x; }
 __device__ inline void store4(u16 *p, f32x4 x) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
 __device__ inline void store4(float *p, f32x4 x) { *reinterpret_cast<f32x4 *>(p) = x; }
 
-// operand straight from a tensor's row (zeros where !ok): 8 values from p on
+// operand straight from a tensor's row, 8 values from p on (a valid address in any case); zeros where !ok
 __device__ inline Op<1> frag_g(const u16 *p, bool ok)
 {
-    u32x4 w = {0, 0, 0, 0};
-    if (ok) w = *reinterpret_cast<const u32x4 *>(p);
+    u32x4 w = *reinterpret_cast<const u32x4 *>(p);
+    w = ok ? w : u32x4{0, 0, 0, 0};
     return Op<1>{{__builtin_bit_cast(bf16x8, w)}};
+}
+template <int P>
+__device__ inline Op<P> op_of(f32x4 x, f32x4 y)
+{
+    u32x2 a[P], b[P];
+    split4<P>(x, a);
+    split4<P>(y, b);
+    Op<P> f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) f.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[i].x, a[i].y, b[i].x, b[i].y});
+    return f;
 }
 __device__ inline Op<3> frag_g(const float *p, bool ok)
 {
-    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-    if (ok) { x = *reinterpret_cast<const f32x4 *>(p); y = *reinterpret_cast<const f32x4 *>(p + 4); }
-    u32x2 a[3], b[3];
-    split4<3>(x, a);
-    split4<3>(y, b);
-    Op<3> f;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) f.p[i] = __builtin_bit_cast(bf16x8, u32x4{a[i].x, a[i].y, b[i].x, b[i].y});
-    return f;
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p), y = *reinterpret_cast<const f32x4 *>(p + 4), z = {0.f, 0.f, 0.f, 0.f};
+    return op_of<3>(ok ? x : z, ok ? y : z);
 }
 
 // 64 rows x D of a tensor on their way to an LDS tile: 256 threads load them into registers, and put them down later
@@ -138,8 +167,8 @@ template <typename T, int D> struct Tile64 {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int row = i * RPP + tid / LPR;
-            r[i] = u32x4{0, 0, 0, 0};
-            if (row < valid) r[i] = *reinterpret_cast<const u32x4 *>(base + (size_t)row * D + tid % LPR * PER);
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(base + (size_t)min(row, valid - 1) * D + tid % LPR * PER);
+            r[i] = row < valid ? w : u32x4{0, 0, 0, 0};
         }
     }
     __device__ inline void store(u16 *tile, int tid) const
@@ -155,8 +184,9 @@ template <typename T, int D> struct Tile64 {
 
 }  // namespace
 
-// per token of a chunk, for the kernels behind delta_chunk_kernel (zeros for tokens that are not there)
-struct DeltaGate { float gamma, tail, beta, pad; };     // exp(b_i), exp(b_63 - b_i), beta_i with b the running sum of g
+// of a chunk, for the kernels behind delta_chunk_kernel, by token: gamma = exp(b_i), tail = exp(b_63 - b_i), beta_i with b the running sum of g
+// (tail and beta are zero for tokens that are not there)
+struct DeltaGate { float gamma[64], tail[64], beta[64]; };
 constexpr int DELTA_C = 64;
 constexpr size_t DELTA_T_ELEMS = 3 * 4 * 2 * 64 * 8;    // T of a chunk: planes, row tiles, halves of the contraction, lanes, 8 each
 
