@@ -92,10 +92,13 @@ struct DeltaArgs {
     float scale;
     int chunks;                     // of 64 tokens
     // workspace, by (sample, head, chunk of 64 tokens)
-    u16 *tf, *ttf;                  // T = (I + A)^-1 and (backward) its transpose: three bf16 planes in operand order
     struct DeltaGate *gate;
     float2 *bsum;                   // [64] each: running sum of g as two floats
-    u16 *pf;                        // forward: P in operand order, one plane for bf16 tensors, three for fp32
+    u16 *tf, *ttf;                  // T = (I + A)^-1 and (backward) its transpose, operands in three planes
+    u16 *pf;                        // forward: P, operand in one plane for bf16 tensors, three for fp32
+    int groups, per_group;          // the chunks are cut into groups whose chains run side by side
+    float *gsum, *gmap, *gstart;    // [BH][groups][D][D]: a group's chain from zeros, its linear map, and the state it starts from
+    float *gsum_b, *gstart_b;       // backward: the same of the gradients' chain (its map is the transpose)
     // backward: what the gradients need of the forward pass
     float *s0;                      // [D][D] the state before the chunk, transposed (value channel, key channel)
     float *u;                       // [D][64] u, transposed
@@ -106,7 +109,6 @@ struct DeltaArgs {
     float *dg, *dbeta, *dstate_in;
     float *ds1;                     // [D][D] gradient of the state behind the chunk, transposed
     float *dr;                      // [D][64] first X = P^T dout, then dR = T^T du, transposed
-    float *dbv;                     // [D/16][64] sums of dR v over 16 value channels
     float *dq_part, *dk_part;       // [B,H,N,D] where heads share queries and keys, else null
 };
 __host__ __device__ inline int delta_len(const DeltaArgs &a, int b)
@@ -117,8 +119,9 @@ __host__ __device__ inline int delta_len(const DeltaArgs &a, int b)
 bool delta_takes_step(const DeltaArgs &a);
 hipError_t launch_delta_step(const DeltaArgs &a, hipStream_t st);
 // steps shared by both directions
-hipError_t launch_delta_chunk(const DeltaArgs &a, hipStream_t st);
+hipError_t launch_delta_chunk(const DeltaArgs &a, bool backward, hipStream_t st);
 hipError_t launch_delta_chains(const DeltaArgs &a, bool backward, hipStream_t st);
+int delta_groups(const DeltaArgs &a, bool backward);      // how many groups of chunks
 hipError_t launch_delta_fwd(const DeltaArgs &a, hipStream_t st);
 hipError_t launch_delta_bwd(const DeltaArgs &a, hipStream_t st);
 

@@ -137,18 +137,29 @@ size_t delta_ws(DeltaArgs &a, bool backward, char *ws)
     const size_t BH = (size_t)a.B * a.H, n = BH * a.chunks, D = a.D;
     size_t off = 0;
     auto take = [&](auto *&to, size_t bytes) { to = (std::remove_reference_t<decltype(to)>)(ws + off); off = align256(off + bytes); };
-    take(a.tf, n * DELTA_T_ELEMS * sizeof(u16));
     take(a.gate, n * sizeof(DeltaGate));
     take(a.bsum, n * 64 * sizeof(float2));
+    take(a.tf, n * 3 * TRI * sizeof(u16));
+    a.groups = delta_groups(a, backward);
+    a.per_group = (a.chunks + a.groups - 1) / a.groups;
+    if (a.groups > 1) {
+        const size_t each = BH * a.groups * D * D * sizeof(float);
+        take(a.gsum, each);
+        take(a.gmap, each);
+        take(a.gstart, each);
+        if (backward) {
+            take(a.gsum_b, each);
+            take(a.gstart_b, each);
+        }
+    }
     if (!backward) {
-        take(a.pf, n * (a.bf16 ? 1 : 3) * 4 * 2 * 64 * 8 * sizeof(u16));
+        take(a.pf, n * (a.bf16 ? 1 : 3) * TRI * sizeof(u16));
     } else {
+        take(a.ttf, n * 3 * TRI * sizeof(u16));
         take(a.s0, n * D * D * sizeof(float));
         take(a.u, n * D * 64 * sizeof(float));
-        take(a.ttf, n * DELTA_T_ELEMS * sizeof(u16));
         take(a.ds1, n * D * D * sizeof(float));
         take(a.dr, n * D * 64 * sizeof(float));
-        take(a.dbv, n * D / 16 * 64 * sizeof(float));
         if (a.H != a.Hk) {
             take(a.dq_part, BH * a.N * D * sizeof(float));
             take(a.dk_part, BH * a.N * D * sizeof(float));

@@ -1,16 +1,18 @@
 // The chains of the gated delta rule: the states from the first chunk to the last, and their gradients from the last to the first
-// (delta_chunk.hip and delta_grad.hip have the formulas).  The value channels are independent: a workgroup takes 16 of one (sample,
-// head).  Its first 4 waves carry the chain, each with D / 4 key channels of the state in accumulators; a chunk is
-//   1. K S: every wave its own channels' share for all 64 tokens, straight from the accumulators, which are an operand as they stand
-//      (the order of a contraction is free, so K's operand takes the channels in theirs); the shares meet in LDS
-//   2. T R: 16 tokens a wave, R from LDS
-//   3. S <- gamma S + K^T (tail u): u from LDS, K^T by transposing reads
-// Its other 4 waves, one on each SIMD beside a wave of the chain, do what the chain does not wait for: they bring the next chunk's K,
-// and forward compute O = scale gamma Q S + P u, backward Q^T (scale gamma dO), dv and the sums of dR v.
-// Three exchanges through LDS and 36 products deep, the chain is bound by their latency, not by memory.  Operands of the next chunk are loaded a
-// chunk ahead into a second set of registers, the barriers wait for LDS alone, and stores are never skipped by a branch, so that no
-// wait for a load waits for a store.
+// (delta_chunk.hip and delta_grad.hip have the formulas).  The value channels are independent, and a wave takes 16 of them with the whole
+// state, D key channels, in accumulators.  A chunk is
+//   K S,   R = beta (V - gamma K S),   U = T R,   S <- gamma_63 S + K^T (tail U)
+// (backward: dU = X + tail K dS, dR = T^T dU, dS <- gamma_63 dS + Q^T (scale gamma dO) - K^T (beta gamma dR)), and what one product leaves in the
+// accumulators is an operand of the next as it stands (delta_planes.h): the chain never leaves its wave's registers.  What all waves
+// read, K, T, V and the decays, lies in LDS, a chunk's while the next one's is on its way: 4 more waves, one on each SIMD, load it, and
+// forward compute O = scale gamma Q S + P U from the operands that the chain leaves behind.
+// 132 products deep (d = 128; backward 180), the chain is bound by the matrix cores' issue: 16 cycles each, one wave to a SIMD.
+//
+// Few heads leave most of the chip idle, so the chunks are cut into groups.  The state behind a group is linear in the one before it,
+// S' = M S + B: chains from zeros give B and chains from the unit matrix without values give M, for all groups at once; a short
+// kernel goes through the groups, and then every group runs from its own state.  The gradients' map is M transposed.
 #include <algorithm>
+#include <type_traits>
 
 #include "causal.h"
 #include "delta_planes.h"
@@ -19,75 +21,67 @@ namespace salad {
 
 namespace {
 
-constexpr int UP = 72;      // pitch of the exchanges' tiles: 64 tokens, 16 bytes aside
+enum Kind { OUT, KEEP, SUM };       // forward call: the output; backward call: states and u, or dS and dR, are kept; a group's B or M alone
 
-template <typename T, int D> struct ChainLds {
-    static constexpr int P = planes_of<T>(), OP = D / 4 + (P == 1 ? 8 : 4), OWN = P * 64 * OP;     // a wave's channels of K or Q: [64 tokens][D / 4]
-    static constexpr int KBUFS = P == 1 ? 2 : 1, QP = D + 8, QT = P * 16 * QP;                    // a wave's tokens of Q: [16 tokens][D]
-    union {
-        f32x4 ks[4][4][64];             // by wave: its share of K S, by row tile and lane
-        f32x4 y[4][4][64];              // backward: Q^T (scale gamma dO) for the wave's channels, once the shares are read
-    };
-    union {
-        struct { u16 q[4][QT]; u32x4 so[4][P][64]; } f;         // forward: Q, and the state as an operand
-        struct { u16 q[4][OWN]; f32x4 dr[4][64]; } b;           // backward: Q, and dR
-    };
-    u16 k[KBUFS][4][OWN];
-    u16 r[3 * 16 * UP], u[3 * 16 * UP], g[3 * 16 * UP];
+template <typename T, int D, bool BACK> struct Shape {
+    static constexpr int P = planes_of<T>();
+    static constexpr int SL = P == 1 ? 4 : 2;                               // waves of the chain, 16 value channels each
+    static constexpr int KBUFS = P == 1 ? 2 : 1;                            // K (and Q) of two chunks, where LDS has room
+    static constexpr int KP = D + 8, VP = 16 * SL + 8, UO = P == 1 ? 1 : 3; // pitches; planes of u as a factor of O
+    static constexpr bool QTILE = BACK || P == 1;                           // Q goes through LDS
+    static constexpr int THREADS = 64 * (SL + 4);
 };
 
-// ROWS rows of W channels of a tensor (a wave's part) on their way to an LDS tile: a wave loads them, 16 bytes a lane, and puts them down later
-template <typename T, int D, int ROWS, int W, int PITCH> struct Part {
-    static constexpr int P = planes_of<T>(), PER = 16 / sizeof(T), LPR = W / PER, RPI = 64 / LPR, NL = ROWS / RPI;
+template <typename T, int D, bool BACK> struct ChainLds {
+    using H = Shape<T, D, BACK>;
+    u16 k[H::KBUFS][H::P * 64 * H::KP];
+    u16 q[BACK ? H::KBUFS : 1][H::QTILE ? H::P * 64 * H::KP : 8];
+    u16 t[3 * TRI];
+    T v[64][H::VP];                             // values; backward: dO
+    float gamma[64], tail[64], beta[64];
+    struct Side { u32x4 so[H::SL][D / 32][H::P][64], uo[H::SL][2][H::UO][64]; };
+    Side side[BACK ? 0 : 2];                    // the state and u as operands, for O a chunk later
+};
+
+// a 64 x 16 SL part of V or dO
+template <typename T, int D, int W, int PITCH> struct Vals {
+    static constexpr int PER = 16 / sizeof(T), LPR = W / PER, RPI = 256 / LPR, NL = (64 + RPI - 1) / RPI;
     u32x4 r[NL];
-    __device__ inline void load(const T *base, int r0, int last, int lane)      // rows r0.., none behind `last`
+    __device__ inline void load(const T *base, int last, int t)
     {
 #pragma unroll
-        for (int i = 0; i < NL; ++i)
-            r[i] = *reinterpret_cast<const u32x4 *>(base + (unsigned)(min(r0 + i * RPI + lane / LPR, last) * D + lane % LPR * PER));
+        for (int i = 0; i < NL; ++i) r[i] = *reinterpret_cast<const u32x4 *>(base + (unsigned)(min(i * RPI + t / LPR, last) * D + t % LPR * PER));
     }
-    __device__ inline void put(u16 *tile, int lane) const
+    __device__ inline void put(T (*tile)[PITCH], int t, int valid) const    // zeros behind the last token
     {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-            u16 *at = tile + (i * RPI + lane / LPR) * PITCH + lane % LPR * PER;
-            if constexpr (P == 1) *reinterpret_cast<u32x4 *>(at) = r[i];
-            else put4<3>(at, ROWS * PITCH, __builtin_bit_cast(f32x4, r[i]));
+            const int row = i * RPI + t / LPR;
+            if (NL * RPI == 64 || row < 64) *reinterpret_cast<u32x4 *>(&tile[row][t % LPR * PER]) = row < valid ? r[i] : u32x4{0, 0, 0, 0};
         }
     }
 };
 
-// operand from a tile's row, the channels in the order of the accumulators: lane group l4 has 4 l4.. of the first 16 channels from c0 on and
-// 4 l4.. of the second (NT = 1: there is none; zeros)
-template <int P, int NT>
-__device__ inline Op<P> frag_own(const u16 *tile, int plane, int pitch, int row, int c0, int l4)
-{
-    Op<P> f;
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const u16 *at = tile + p * plane + row * pitch + c0 + 4 * l4;
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(at), y = NT > 1 ? *reinterpret_cast<const u32x2 *>(at + 16) : u32x2{0, 0};
-        f.p[p] = __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
-    }
-    return f;
-}
-
-// 4 tokens of a value channel, loaded as they are and converted later
-template <typename T> struct Four {
-    T r[4];
-    __device__ inline void load(const T *base, int stride, int t0, int last, int c)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = base[(unsigned)(min(t0 + i, last) * stride + c)];
-    }
-    __device__ inline f32x4 get(int t0, int valid) const    // zeros behind the last token
-    {
-        f32x4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = t0 + i < valid ? load1(&r[i]) : 0.f;
-        return x;
-    }
+// where a workgroup works: value channels from c0 on, chunks [first, end) of the sample
+struct Job {
+    int bh, group, c0, len, first, end;
+    bool unit;                                  // SUM: the chain from the unit matrix
 };
+
+__device__ inline f32x4 values(const u16 (*v)[72], int row, int c, int lane)    // rows row + 4 (lane / 16).., column c + lane % 16
+{
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (s16x4 __attribute__((address_space(3))) *)LDS_PTR(&v[row + 4 * (lane >> 4) + ((lane >> 2) & 3)][c + 4 * (lane & 3)]));
+    return f32x4{__uint_as_float((uint32_t)(u16)x[0] << 16), __uint_as_float((uint32_t)(u16)x[1] << 16), __uint_as_float((uint32_t)(u16)x[2] << 16),
+                 __uint_as_float((uint32_t)(u16)x[3] << 16)};
+}
+__device__ inline f32x4 values(const float (*v)[40], int row, int c, int lane)
+{
+    f32x4 x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = v[row + 4 * (lane >> 4) + r][c + (lane & 15)];
+    return x;
+}
 
 template <int P>
 __device__ inline Op<P> first_planes(const Op<3> &f)
@@ -97,428 +91,402 @@ __device__ inline Op<P> first_planes(const Op<3> &f)
     for (int i = 0; i < P; ++i) o.p[i] = f.p[i];
     return o;
 }
-
-// the accumulators of the wave's channels as an operand
-template <int NT>
-__device__ inline Op<3> state_op(const f32x4 (&s)[NT])
+__device__ inline Op<3> tri_op(const u16 *t, int piece, int lane)
 {
-    const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-    return op_of<3>(s[0], NT > 1 ? s[NT - 1] : z);
-}
-
-template <int P>
-__device__ inline Op<P> packed_op(const u16 *from, int w, int kt, int lane)
-{
-    Op<P> f;
+    Op<3> f;
 #pragma unroll
-    for (int p = 0; p < P; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(from + (((p * 4 + w) * 2 + kt) * 64 + lane) * 8);
+    for (int p = 0; p < 3; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(t + p * TRI + (piece * 64 + lane) * 8);
     return f;
 }
 
-// where a workgroup and a lane of it work
-template <typename T, int D> struct Place {
-    int bh, slice, c0, len, chunks, lane, w, l16, l4, arow, i0;     // arow, i0: first of an accumulator's 4 key channels, 4 tokens
-    const T *k, *q;                                                 // of the head
-    __device__ Place(const DeltaArgs &a, int bh_, int slice_, int w_) : bh(bh_), slice(slice_), c0(slice_ * 16), w(w_)
-    {
-        const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
-        len = delta_len(a, b);
-        chunks = (len + 63) / 64;
-        lane = threadIdx.x & 63;
-        l16 = lane & 15;
-        l4 = lane >> 4;
-        arow = w * (D / 4) + 4 * l4;
-        i0 = 16 * w + 4 * l4;
-        k = reinterpret_cast<const T *>(a.k) + ((size_t)b * a.Hk + hk) * a.N * D;
-        q = reinterpret_cast<const T *>(a.q) + ((size_t)b * a.Hk + hk) * a.N * D;
+// Barriers of both roles: before the first chunk; in a chunk behind T R (T, V and the decays are free), where K has one buffer behind
+// the products with it, and at its end (the next chunk's operands are there).
+
+template <typename T, int D, bool BACK, Kind KIND>
+__device__ inline void chain(const DeltaArgs &a, const Job &j, ChainLds<T, D, BACK> &lds, int w, int lane)
+{
+    using H = Shape<T, D, BACK>;
+    constexpr int P = H::P, NK = D / 32, KP = H::KP;
+    const int l16 = lane & 15, l4 = lane >> 4, c = j.c0 + 16 * w + l16, n = j.end - j.first;
+    const bool unit = KIND == SUM && !BACK && j.unit;       // the chain from the unit matrix, without values
+    f32x4 s[NK][2];
+    // state: key channel 32 ks + 8 l4 + 4 x + r, value channel c
+    const float *from = KIND == SUM ? nullptr : a.groups > 1 ? (BACK ? a.gstart_b : a.gstart) + ((size_t)j.bh * a.groups + j.group) * D * D
+                                                             : BACK ? a.dstate_out + (a.dstate_out ? (size_t)j.bh * D * D : 0)
+                                                                    : a.state_in + (a.state_in ? (size_t)j.bh * D * D : 0);
+    const bool first_group = BACK ? j.group == a.groups - 1 : j.group == 0;
+    if (KIND == SUM && first_group) {           // nothing is before it: its B is the state behind it
+        const float *in = BACK ? a.dstate_out : a.state_in;
+        from = in ? in + (size_t)j.bh * D * D : nullptr;
     }
-    __device__ int last(int ch) const { return min(len - ch * 64, 64) - 1; }
-    __device__ size_t at(const DeltaArgs &a, int ch) const { return (size_t)bh * a.chunks + ch; }
-    __device__ size_t rows(const DeltaArgs &a, int ch) const { return ((size_t)bh * a.N + (size_t)ch * 64) * D; }
-};
-
-template <typename T, int D>
-__device__ inline void load_state(const float *from, const Place<T, D> &p, f32x4 (&s)[D / 64])
-{
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x)
+    for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[x][r] = from ? from[((size_t)p.bh * D + p.arow + 16 * x + r) * D + p.c0 + p.l16] : 0.f;
-}
-template <typename T, int D>
-__device__ inline void store_state(float *to, const Place<T, D> &p, const f32x4 (&s)[D / 64])
-{
-    if (!to) return;
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) to[((size_t)p.bh * D + p.arow + 16 * x + r) * D + p.c0 + p.l16] = s[x][r];
-}
-
-// Barriers of both roles: one before the first chunk (K of it is there), three in a chunk, and a fourth where K has one buffer only.
-
-// ---- forward.  OUT: the layer's output; else what the gradients need (the states and u) ----------------------------
-template <typename T, int D, bool OUT>
-__device__ inline void forward_chain(const DeltaArgs &a, const Place<T, D> p, ChainLds<T, D> &lds)
-{
-    using L = ChainLds<T, D>;
-    constexpr int P = L::P, NT = D / 64, UO = P == 1 ? 2 : 3;               // planes of u as a factor of O
-    f32x4 s[NT];
-    load_state(a.state_in, p, s);
-    struct In {
-        Op<3> t[2];
-        Four<T> v;
-        f32x4 gamma, tail, beta;
-        float end;
-    } in0, in1;
-    auto fetch = [&](In &n, int ch) __attribute__((always_inline)) {
-        const size_t at = p.at(a, ch);
-        const DeltaGate &gate = a.gate[at];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) n.t[kt] = packed_op<3>(a.tf + at * DELTA_T_ELEMS, p.w, kt, p.lane);
-        n.v.load(reinterpret_cast<const T *>(a.v) + p.rows(a, ch), D, p.i0, p.last(ch), p.c0 + p.l16);
-        n.gamma = load4(gate.gamma + p.i0);
-        n.tail = load4(gate.tail + p.i0);
-        n.beta = load4(gate.beta + p.i0);
-        n.end = gate.gamma[63];
-    };
-    if (!p.chunks) { store_state(a.state_out, p, s); return; }
-    Op<P> k[4];
-    auto take_k = [&](int ch) __attribute__((always_inline)) {
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) k[rt] = frag_own<P, NT>(lds.k[ch & (L::KBUFS - 1)][p.w], 64 * L::OP, L::OP, 16 * rt + p.l16, 0, p.l4);
-    };
-    fetch(in0, 0);
-    lds_barrier();
-    take_k(0);
-    auto step = [&](const In &in, In &next, int ch) __attribute__((always_inline)) {
-        const size_t at = p.at(a, ch);
-        const u16 *K = lds.k[ch & (L::KBUFS - 1)][p.w];
-        const Op<3> so = state_op(s);
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            f32x4 c = {0.f, 0.f, 0.f, 0.f};
-            mma(c, k[rt], so);
-            lds.ks[p.w][rt][p.lane] = c;
-        }
-        if (OUT)
-#pragma unroll
-            for (int i = 0; i < P; ++i) lds.f.so[p.w][i][p.lane] = __builtin_bit_cast(u32x4, so.p[i]);
-        lds_barrier();
-        f32x4 ks = lds.ks[0][p.w][p.lane], rr;
-#pragma unroll
-        for (int w = 1; w < 4; ++w) ks += lds.ks[w][p.w][p.lane];
-        if (!OUT)
-#pragma unroll
-            for (int x = 0; x < NT; ++x) store4(a.s0 + (at * D + p.c0 + p.l16) * D + p.arow + 16 * x, s[x]);
-        const f32x4 v = in.v.get(p.i0, p.last(ch) + 1);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) rr[r] = in.beta[r] * (v[r] - in.gamma[r] * ks[r]);
-        put4<3>(lds.r + p.l16 * UP + p.i0, 16 * UP, rr);
-        lds_barrier();
-        const Op<3> r0 = frag_n<3>(lds.r, 16 * UP, UP, 0, 0, p.lane), r1 = frag_n<3>(lds.r, 16 * UP, UP, 0, 32, p.lane);
-        Op<P> kt[NT][2];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            kt[x][0] = frag_t<P>(K, 64 * L::OP, L::OP, 16 * x, 0, p.lane);
-            kt[x][1] = frag_t<P>(K, 64 * L::OP, L::OP, 16 * x, 32, p.lane);
-        }
-        fetch(next, min(ch + 1, p.chunks - 1));
-        f32x4 u = {0.f, 0.f, 0.f, 0.f};
-        mma(u, in.t[0], r0);
-        if (p.w >= 2) mma(u, in.t[1], r1);                              // T is lower triangular
-        f32x4 ut;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) ut[r] = u[r] * in.tail[r];
-        put4<3>(lds.u + p.l16 * UP + p.i0, 16 * UP, ut);
-        if (OUT) put4<UO>(lds.g + p.l16 * UP + p.i0, 16 * UP, u);
-        else store4(a.u + (at * D + p.c0 + p.l16) * 64 + p.i0, u);
-        lds_barrier();
-        const Op<3> u0 = frag_n<3>(lds.u, 16 * UP, UP, 0, 0, p.lane), u1 = frag_n<3>(lds.u, 16 * UP, UP, 0, 32, p.lane);
-        if (L::KBUFS > 1) take_k(ch + 1);
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            s[x] *= in.end;
-            mma(s[x], kt[x][0], u0);
-            mma(s[x], kt[x][1], u1);
-        }
-        if (L::KBUFS == 1) { lds_barrier(); take_k(ch + 1); }
-    };
-    for (int ch = 0; ch < p.chunks; ch += 2) {
-        step(in0, in1, ch);
-        if (ch + 1 < p.chunks) step(in1, in0, ch + 1);
-    }
-    store_state(a.state_out, p, s);
-}
-
-template <typename T, int D, bool OUT>
-__device__ inline void forward_helper(const DeltaArgs &a, const Place<T, D> p, ChainLds<T, D> &lds)
-{
-    using L = ChainLds<T, D>;
-    constexpr int P = L::P, NT = D / 64, UO = P == 1 ? 2 : 3;
-    if (!p.chunks) return;
-    Part<T, D, 64, D / 4, L::OP> kn;
-    Part<T, D, 16, D, L::QP> qn;
-    struct In {
-        Op<P> pf[2];
-        f32x4 gamma;
-    } in0, in1;
-    u16 *Q = lds.f.q[p.w];
-    auto fetch_rows = [&](int ch) __attribute__((always_inline)) {
-        kn.load(p.k + (size_t)ch * 64 * D + p.w * (D / 4), 0, p.last(ch), p.lane);
-        if (OUT) qn.load(p.q + (size_t)ch * 64 * D, 16 * p.w, p.last(ch), p.lane);
-    };
-    auto fetch = [&](In &n, int ch) __attribute__((always_inline)) {
-        if (!OUT) return;
-        const size_t at = p.at(a, ch);
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) n.pf[kt] = packed_op<P>(a.pf + at * (P * 4096), p.w, kt, p.lane);
-        n.gamma = load4(a.gate[at].gamma + p.i0);
-    };
-    fetch_rows(0);
-    fetch(in0, 0);
-    kn.put(lds.k[0][p.w], p.lane);
-    if (OUT) qn.put(Q, p.lane);
-    lds_barrier();
-    auto step = [&](const In &in, In &next, int ch) __attribute__((always_inline)) {
-        fetch_rows(min(ch + 1, p.chunks - 1));
-        fetch(next, min(ch + 1, p.chunks - 1));
-        Op<P> q[4];
-        if (OUT)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) q[g] = frag_own<P, NT>(Q, 16 * L::QP, L::QP, p.l16, g * (D / 4), p.l4);
-        lds_barrier();
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        if (OUT)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                Op<P> so;
-#pragma unroll
-                for (int i = 0; i < P; ++i) so.p[i] = __builtin_bit_cast(bf16x8, lds.f.so[g][i][p.lane]);
-                mma(o, q[g], so);
+            for (int r = 0; r < 4; ++r) {
+                const int row = 32 * ks + 8 * l4 + 4 * x + r;
+                s[ks][x][r] = unit ? (row == c ? 1.f : 0.f) : from ? from[(size_t)row * D + c] : 0.f;
             }
-        lds_barrier();
-        if (L::KBUFS > 1) kn.put(lds.k[(ch + 1) & 1][p.w], p.lane);
-        lds_barrier();
-        if (L::KBUFS == 1) { kn.put(lds.k[0][p.w], p.lane); lds_barrier(); }
-        if (OUT) {
+    f32x4 x[4];                                 // backward: X = P^T dO of the next chunk
+    auto load_x = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] *= a.scale * in.gamma[r];
-            mma(o, in.pf[0], frag_n<UO>(lds.g, 16 * UP, UP, 0, 0, p.lane));
-            if (p.w >= 2) mma(o, in.pf[1], frag_n<UO>(lds.g, 16 * UP, UP, 0, 32, p.lane));       // P is lower triangular
-            const auto rows = bounded(reinterpret_cast<T *>(a.out) + p.rows(a, ch), (p.last(ch) + 1) * D);
+        for (int rt = 0; rt < 4; ++rt) x[rt] = load4(a.dr + (((size_t)j.bh * a.chunks + j.end - 1 - i) * D + c) * 64 + 16 * rt + 4 * l4);
+    };
+    if (BACK && n > 0) load_x(0);
+    if (n > 0) lds_barrier();
+    for (int i = 0; i < n; ++i) {
+        const int ch = BACK ? j.end - 1 - i : j.first + i;
+        const size_t at = (size_t)j.bh * a.chunks + ch;
+        const u16 *K = lds.k[i & (H::KBUFS - 1)], *Q = lds.q[BACK ? i & (H::KBUFS - 1) : 0];
+        if (KIND == KEEP)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) store_bounded(rows, T(), (p.i0 + r) * D + p.c0 + p.l16, o[r]);
-            qn.put(Q, p.lane);
+            for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) store4((BACK ? a.ds1 : a.s0) + (at * D + c) * D + 32 * ks + 8 * l4 + 4 * y, s[ks][y]);
+        f32x4 acc[4];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+            const Op<3> so = op_of<3>(s[ks][0], s[ks][1]);
+            if constexpr (KIND == OUT)
+#pragma unroll
+                for (int p = 0; p < P; ++p) lds.side[i & 1].so[w][ks][p][lane] = __builtin_bit_cast(u32x4, so.p[p]);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) mma(acc[rt], frag_n<P>(K, 64 * KP, KP, 16 * rt, 32 * ks, lane), so);
         }
-    };
-    for (int ch = 0; ch < p.chunks; ch += 2) {
-        step(in0, in1, ch);
-        if (ch + 1 < p.chunks) step(in1, in0, ch + 1);
-    }
-}
-
-// ---- backward: the states' gradients; also dR, dv, and the sums of dR v that dbeta takes ---------------------------
-template <typename T, int D>
-__device__ inline void backward_chain(const DeltaArgs &a, const Place<T, D> p, ChainLds<T, D> &lds)
-{
-    using L = ChainLds<T, D>;
-    constexpr int P = L::P, NT = D / 64;
-    f32x4 s[NT];
-    load_state(a.dstate_out, p, s);
-    struct In {
-        Op<3> t[2];
-        f32x4 gamma, tail, beta, x;
-        float end;
-    } in0, in1;
-    auto fetch = [&](In &n, int ch) __attribute__((always_inline)) {
-        const size_t at = p.at(a, ch);
-        const DeltaGate &gate = a.gate[at];
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) n.t[kt] = packed_op<3>(a.ttf + at * DELTA_T_ELEMS, p.w, kt, p.lane);
-        n.x = load4(a.dr + (at * D + p.c0 + p.l16) * 64 + p.i0);
-        n.gamma = load4(gate.gamma + p.i0);
-        n.tail = load4(gate.tail + p.i0);
-        n.beta = load4(gate.beta + p.i0);
-        n.end = gate.gamma[63];
-    };
-    if (!p.chunks) { store_state(a.dstate_in, p, s); return; }
-    Op<P> k[4];
-    auto take_k = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) k[rt] = frag_own<P, NT>(lds.k[i & (L::KBUFS - 1)][p.w], 64 * L::OP, L::OP, 16 * rt + p.l16, 0, p.l4);
-    };
-    fetch(in0, p.chunks - 1);
-    lds_barrier();
-    take_k(0);
-    auto step = [&](const In &in, In &next, int i) __attribute__((always_inline)) {
-        const int ch = p.chunks - 1 - i;
-        const size_t at = p.at(a, ch);
-        const u16 *K = lds.k[i & (L::KBUFS - 1)][p.w];
-        const Op<3> so = state_op(s);
+        // R, or dU
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
-            f32x4 c = {0.f, 0.f, 0.f, 0.f};
-            mma(c, k[rt], so);
-            lds.ks[p.w][rt][p.lane] = c;
+            if (BACK) {
+                const f32x4 tail = load4(lds.tail + 16 * rt + 4 * l4);
+                acc[rt] = x[rt] + tail * acc[rt];
+            } else {
+                const f32x4 gamma = load4(lds.gamma + 16 * rt + 4 * l4), beta = load4(lds.beta + 16 * rt + 4 * l4);
+                if (unit) acc[rt] = -beta * gamma * acc[rt];
+                else acc[rt] = beta * (values(lds.v, 16 * rt, 16 * w, lane) - gamma * acc[rt]);
+            }
         }
-        lds_barrier();
-        f32x4 du = lds.ks[0][p.w][p.lane];
+        if (BACK) load_x(min(i + 1, n - 1));
+        const Op<3> r0 = op_of<3>(acc[0], acc[1]), r1 = op_of<3>(acc[2], acc[3]);
+        f32x4 u[4];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) du += lds.ks[w][p.w][p.lane];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) store4(a.ds1 + (at * D + p.c0 + p.l16) * D + p.arow + 16 * x, s[x]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) du[r] = in.x[r] + in.tail[r] * du[r];
-        put4<3>(lds.r + p.l16 * UP + p.i0, 16 * UP, du);
-        lds_barrier();
-        const Op<3> r0 = frag_n<3>(lds.r, 16 * UP, UP, 0, 0, p.lane), r1 = frag_n<3>(lds.r, 16 * UP, UP, 0, 32, p.lane);
-        Op<P> kt[NT][2];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            kt[x][0] = frag_t<P>(K, 64 * L::OP, L::OP, 16 * x, 0, p.lane);
-            kt[x][1] = frag_t<P>(K, 64 * L::OP, L::OP, 16 * x, 32, p.lane);
+        for (int rt = 0; rt < 4; ++rt) {
+            u[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (BACK ? rt < 2 : true) mma(u[rt], tri_op(lds.t, BACK ? tri_upper(rt, 0) : tri_lower(rt, 0), lane), r0);
+            if (BACK ? true : rt >= 2) mma(u[rt], tri_op(lds.t, BACK ? tri_upper(rt, 1) : tri_lower(rt, 1), lane), r1);
         }
-        fetch(next, max(ch - 1, 0));
-        f32x4 dr = {0.f, 0.f, 0.f, 0.f}, w;
-        if (p.w < 2) mma(dr, in.t[0], r0);                              // T^T is upper triangular
-        mma(dr, in.t[1], r1);
+        if constexpr (KIND == OUT) {
+            const Op<H::UO> u0 = op_of<H::UO>(u[0], u[1]), u1 = op_of<H::UO>(u[2], u[3]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = -in.gamma[r] * in.beta[r] * dr[r];
-        put4<3>(lds.u + p.l16 * UP + p.i0, 16 * UP, w);
-        lds.b.dr[p.w][p.lane] = dr;
-        lds_barrier();
-        const Op<3> w0 = frag_n<3>(lds.u, 16 * UP, UP, 0, 0, p.lane), w1 = frag_n<3>(lds.u, 16 * UP, UP, 0, 32, p.lane);
-        f32x4 y[NT];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) y[x] = lds.y[p.w][x][p.lane];
-        if (L::KBUFS > 1) take_k(i + 1);
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            s[x] = s[x] * in.end + y[x];
-            mma(s[x], kt[x][0], w0);
-            mma(s[x], kt[x][1], w1);
+            for (int p = 0; p < H::UO; ++p) {
+                lds.side[i & 1].uo[w][0][p][lane] = __builtin_bit_cast(u32x4, u0.p[p]);
+                lds.side[i & 1].uo[w][1][p][lane] = __builtin_bit_cast(u32x4, u1.p[p]);
+            }
         }
-        if (L::KBUFS == 1) { lds_barrier(); take_k(i + 1); }
-    };
-    for (int i = 0; i < p.chunks; i += 2) {
-        step(in0, in1, i);
-        if (i + 1 < p.chunks) step(in1, in0, i + 1);
+        if (KIND == KEEP)
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) store4((BACK ? a.dr : a.u) + (at * D + c) * 64 + 16 * rt + 4 * l4, u[rt]);
+        Op<3> g0, g1;
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+            if (BACK) {
+                const f32x4 gamma = load4(lds.gamma + 16 * rt + 4 * l4), beta = load4(lds.beta + 16 * rt + 4 * l4);
+                acc[rt] = a.scale * gamma * values(lds.v, 16 * rt, 16 * w, lane);
+                u[rt] *= -beta * gamma;
+            } else {
+                u[rt] *= load4(lds.tail + 16 * rt + 4 * l4);
+            }
+        }
+        if (BACK) { g0 = op_of<3>(acc[0], acc[1]); g1 = op_of<3>(acc[2], acc[3]); }
+        const Op<3> u0 = op_of<3>(u[0], u[1]), u1 = op_of<3>(u[2], u[3]);
+        const float end = lds.gamma[63];
+        lds_barrier();
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                s[ks][y] *= end;
+                if (BACK) {
+                    mma(s[ks][y], frag_c<P>(Q, 64 * KP, KP, ks, y, 0, lane), g0);
+                    mma(s[ks][y], frag_c<P>(Q, 64 * KP, KP, ks, y, 1, lane), g1);
+                }
+                mma(s[ks][y], frag_c<P>(K, 64 * KP, KP, ks, y, 0, lane), u0);
+                mma(s[ks][y], frag_c<P>(K, 64 * KP, KP, ks, y, 1, lane), u1);
+            }
+        if (H::KBUFS == 1) lds_barrier();
+        lds_barrier();
     }
-    store_state(a.dstate_in, p, s);
+    // the state behind the last chunk
+    const bool last_group = BACK ? j.group == 0 : j.group == a.groups - 1;
+    float *to = KIND == SUM ? (unit ? a.gmap : BACK ? a.gsum_b : a.gsum) + ((size_t)j.bh * a.groups + j.group) * D * D
+                : !last_group ? nullptr : BACK ? (a.dstate_in ? a.dstate_in + (size_t)j.bh * D * D : nullptr) : (a.state_out ? a.state_out + (size_t)j.bh * D * D : nullptr);
+    if (to)
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) to[(size_t)(32 * ks + 8 * l4 + 4 * x + r) * D + c] = s[ks][x][r];
 }
 
-template <typename T, int D>
-__device__ inline void backward_helper(const DeltaArgs &a, const Place<T, D> p, ChainLds<T, D> &lds)
+// The next chunk's operands, and O of the chunk before.  Wave w of 4: 16 tokens of O.
+template <typename T, int D, bool BACK, Kind KIND>
+__device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, BACK> &lds, int w, int lane)
 {
-    using L = ChainLds<T, D>;
-    constexpr int P = L::P, NT = D / 64;
-    if (!p.chunks) return;
-    Part<T, D, 64, D / 4, L::OP> kn, qn;
-    struct In {
-        Four<T> v, o;
-        f32x4 gamma, beta;
-    } in0, in1;
-    u16 *Q = lds.b.q[p.w];
-    auto fetch_rows = [&](int ch) __attribute__((always_inline)) {
-        kn.load(p.k + (size_t)ch * 64 * D + p.w * (D / 4), 0, p.last(ch), p.lane);
-        qn.load(p.q + (size_t)ch * 64 * D + p.w * (D / 4), 0, p.last(ch), p.lane);
+    using H = Shape<T, D, BACK>;
+    constexpr int P = H::P, NK = D / 32, KP = H::KP, SL = H::SL;
+    const int t = w * 64 + lane, l16 = lane & 15, l4 = lane >> 4, n = j.end - j.first;
+    if (n <= 0) return;
+    const int b = j.bh / a.H, h = j.bh - b * a.H, hk = h / (a.H / a.Hk);
+    const T *k = reinterpret_cast<const T *>(a.k) + ((size_t)b * a.Hk + hk) * a.N * D, *q = reinterpret_cast<const T *>(a.q) + ((size_t)b * a.Hk + hk) * a.N * D;
+    const T *v = reinterpret_cast<const T *>(BACK ? a.dout : a.v) + (size_t)j.bh * a.N * D + j.c0;
+    const u16 *tri = BACK ? a.ttf : a.tf;
+    auto chunk_of = [&](int i) { return BACK ? j.end - 1 - i : j.first + i; };
+    auto valid_of = [&](int ch) { return min(j.len - ch * 64, 64); };
+
+    Tile64<T, D> kr, qr;
+    Vals<T, D, 16 * SL, H::VP> vr;
+    u32x4 tr[(3 * TRI / 8 + 255) / 256];
+    float gr = 0.f;
+    constexpr int NT = sizeof(tr) / 16;
+    auto load = [&](int i) __attribute__((always_inline)) {
+        const int ch = chunk_of(i), valid = valid_of(ch);
+        const size_t at = (size_t)j.bh * a.chunks + ch;
+        kr.load(k + (size_t)ch * 64 * D, valid, t);
+        if (BACK) qr.load(q + (size_t)ch * 64 * D, valid, t);
+        vr.load(v + (size_t)ch * 64 * D, valid - 1, t);
+#pragma unroll
+        for (int x = 0; x < NT; ++x) tr[x] = *reinterpret_cast<const u32x4 *>(tri + at * (3 * TRI) + (size_t)min(x * 256 + t, 3 * TRI / 8 - 1) * 8);
+        gr = reinterpret_cast<const float *>(a.gate + at)[min(t, 191)];
     };
-    auto fetch = [&](In &n, int ch) __attribute__((always_inline)) {
-        n.v.load(reinterpret_cast<const T *>(a.v) + p.rows(a, ch), D, p.i0, p.last(ch), p.c0 + p.l16);
-        n.o.load(reinterpret_cast<const T *>(a.dout) + p.rows(a, ch), D, p.i0, p.last(ch), p.c0 + p.l16);
-        n.gamma = load4(a.gate[p.at(a, ch)].gamma + p.i0);
-        n.beta = load4(a.gate[p.at(a, ch)].beta + p.i0);
+    auto put_small = [&](int i) __attribute__((always_inline)) {
+        vr.put(lds.v, t, valid_of(chunk_of(i)));
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+            if ((x + 1) * 256 <= 3 * TRI / 8 || x * 256 + t < 3 * TRI / 8) *reinterpret_cast<u32x4 *>(lds.t + (x * 256 + t) * 8) = tr[x];
+        if (t < 64) lds.gamma[t] = gr;
+        else if (t < 128) lds.tail[t - 64] = gr;
+        else if (t < 192) lds.beta[t - 128] = gr;
     };
-    fetch_rows(p.chunks - 1);
-    fetch(in0, p.chunks - 1);
-    kn.put(lds.k[0][p.w], p.lane);
-    qn.put(Q, p.lane);
+    auto put_rows = [&](int i) __attribute__((always_inline)) {
+        kr.store(lds.k[i & (H::KBUFS - 1)], t);
+        if (BACK) qr.store(lds.q[i & (H::KBUFS - 1)], t);
+    };
+    // O: what it takes besides the chain's operands, loaded in its chunk, used in the next
+    Op<P> pf[2], qn[P == 1 ? 1 : NK];
+    float gamma = 0.f;
+    auto load_out = [&](int i) __attribute__((always_inline)) {
+        const int ch = chunk_of(i), valid = valid_of(ch);
+        const size_t at = (size_t)j.bh * a.chunks + ch;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                pf[kt].p[p] = *reinterpret_cast<const bf16x8 *>(a.pf + at * (P * TRI) + p * TRI + (tri_lower(w, w < 2 ? 0 : kt) * 64 + lane) * 8);
+        gamma = a.scale * a.gate[at].gamma[16 * w + l16];
+        if constexpr (H::QTILE) qr.load(q + (size_t)ch * 64 * D, valid, t);
+        else
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) qn[ks] = frag_g(q + (size_t)(ch * 64 + min(16 * w + l16, valid - 1)) * D + 32 * ks + 8 * l4, true);
+    };
+    auto output = [&](int i) __attribute__((always_inline)) {
+        if constexpr (KIND == OUT) {
+            const int ch = chunk_of(i);
+            const auto &side = lds.side[i & 1];
+            const auto rows = bounded(reinterpret_cast<T *>(a.out) + ((size_t)j.bh * a.N + (size_t)ch * 64) * D, valid_of(ch) * D);
+            Op<P> qo[NK];
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) {
+                if constexpr (H::QTILE) qo[ks] = frag_n<P>(lds.q[0], 64 * KP, KP, 16 * w, 32 * ks, lane);
+                else qo[ks] = qn[ks];
+            }
+#pragma unroll
+            for (int sl = 0; sl < SL; ++sl) {           // transposed: rows value channels, columns tokens
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) {
+                    Op<P> so;
+#pragma unroll
+                    for (int p = 0; p < P; ++p) so.p[p] = __builtin_bit_cast(bf16x8, side.so[sl][ks][p][lane]);
+                    mma(o, so, qo[ks]);
+                }
+                o *= gamma;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    if (kt && w < 2) continue;          // P is lower triangular
+                    Op<H::UO> uo;
+#pragma unroll
+                    for (int p = 0; p < H::UO; ++p) uo.p[p] = __builtin_bit_cast(bf16x8, side.uo[sl][kt][p][lane]);
+                    mma(o, uo, pf[kt]);
+                }
+                store_bounded(rows, T(), (16 * w + l16) * D + j.c0 + 16 * sl + 4 * l4, o);
+            }
+        }
+    };
+
+    load(0);
+    put_rows(0);
+    put_small(0);
     lds_barrier();
-    auto step = [&](const In &in, In &next, int i) __attribute__((always_inline)) {
-        const int ch = p.chunks - 1 - i, valid = p.last(ch) + 1;
-        const size_t at = p.at(a, ch);
-        fetch_rows(max(ch - 1, 0));
-        fetch(next, max(ch - 1, 0));
-        f32x4 go = in.o.get(p.i0, valid);
-        const f32x4 v = in.v.get(p.i0, valid);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) go[r] *= a.scale * in.gamma[r];
-        put4<3>(lds.g + p.l16 * UP + p.i0, 16 * UP, go);
+    for (int i = 0; i < n; ++i) {
+        load(min(i + 1, n - 1));
+        if (KIND == OUT && i > 0) output(i - 1);
+        if (KIND == OUT) load_out(i);
+        if (H::KBUFS > 1) put_rows(i + 1);
         lds_barrier();
-        const Op<3> g0 = frag_n<3>(lds.g, 16 * UP, UP, 0, 0, p.lane), g1 = frag_n<3>(lds.g, 16 * UP, UP, 0, 32, p.lane);
-        f32x4 y[NT];
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-            mma(y[x], frag_t<P>(Q, 64 * L::OP, L::OP, 16 * x, 0, p.lane), g0);
-            mma(y[x], frag_t<P>(Q, 64 * L::OP, L::OP, 16 * x, 32, p.lane), g1);
-        }
+        put_small(min(i + 1, n - 1));
+        if (KIND == OUT && H::QTILE) qr.store(lds.q[0], t);
+        if (H::KBUFS == 1) { lds_barrier(); put_rows(i + 1); }
         lds_barrier();
-#pragma unroll
-        for (int x = 0; x < NT; ++x) lds.y[p.w][x][p.lane] = y[x];
-        if (L::KBUFS > 1) kn.put(lds.k[(i + 1) & 1][p.w], p.lane);
-        lds_barrier();
-        const f32x4 dr = lds.b.dr[p.w][p.lane];
-        if (L::KBUFS == 1) { kn.put(lds.k[0][p.w], p.lane); lds_barrier(); }
-        store4(a.dr + (at * D + p.c0 + p.l16) * 64 + p.i0, dr);
-        const auto rows = bounded(reinterpret_cast<T *>(a.dv) + p.rows(a, ch), valid * D);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            store_bounded(rows, T(), (p.i0 + r) * D + p.c0 + p.l16, in.beta[r] * dr[r]);
-            float d = dr[r] * v[r];                                     // over the 16 channels
-#pragma unroll
-            for (int m = 1; m < 16; m <<= 1) d += __shfl_xor(d, m);
-            a.dbv[(at * (D / 16) + p.slice) * 64 + p.i0 + r] = d;       // the same from all 16 lanes
-        }
-        qn.put(Q, p.lane);
-    };
-    for (int i = 0; i < p.chunks; i += 2) {
-        step(in0, in1, i);
-        if (i + 1 < p.chunks) step(in1, in0, i + 1);
     }
+    if (KIND == OUT) output(n - 1);
 }
 
-// Slices of a head on one XCD, whose L2 then serves K, Q, T and P to all of them.
-__device__ inline int chain_of(int block, int total) { return (block & 7) * ((total + 7) / 8) + (block >> 3); }
+template <typename T, int D, bool BACK, Kind KIND>
+__device__ inline void run(const DeltaArgs &a, const Job &j, ChainLds<T, D, BACK> &lds)
+{
+    constexpr int SL = Shape<T, D, BACK>::SL;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (wave < SL) chain<T, D, BACK, KIND>(a, j, lds, wave, lane);
+    else helper<T, D, BACK, KIND>(a, j, lds, wave - SL, lane);
+}
+
+// Workgroups of a head next to each other, on one XCD: its L2 then serves the operands to all of them
+__device__ inline int place_of(int block, int total) { return (block & 7) * ((total + 7) / 8) + (block >> 3); }
+
+__device__ inline Job job_of(const DeltaArgs &a, int bh, int group, int c0, bool unit)
+{
+    Job j{bh, group, c0, delta_len(a, bh / a.H), 0, 0, unit};
+    const int chunks = (j.len + 63) / 64;
+    j.first = min(group * a.per_group, chunks);
+    j.end = min(j.first + a.per_group, chunks);
+    return j;
+}
 
 }  // namespace
 
+template <typename T, int D> union BothLds {
+    ChainLds<T, D, false> f;
+    ChainLds<T, D, true> b;
+};
+template <typename T, int D> constexpr int PARTS = D / (16 * Shape<T, D, false>::SL);      // workgroups across the value channels
+
 template <typename T, int D>
-__global__ __launch_bounds__(512, 1) void delta_forward_kernel(DeltaArgs a)
+__global__ __launch_bounds__((Shape<T, D, false>::THREADS), 1) void delta_forward_kernel(DeltaArgs a)
 {
-    __shared__ __attribute__((aligned(16))) ChainLds<T, D> lds;
-    const int total = a.B * a.H * (D / 16), L = chain_of(blockIdx.x, total), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) ChainLds<T, D, false> lds;
+    constexpr int NP = PARTS<T, D>;
+    const int total = a.B * a.H * a.groups * NP, L = place_of(blockIdx.x, total);
     if (L >= total) return;
-    const Place<T, D> p(a, L / (D / 16), L % (D / 16), wave & 3);
-    if (wave < 4) forward_chain<T, D, true>(a, p, lds);
-    else forward_helper<T, D, true>(a, p, lds);
+    run<T, D, false, OUT>(a, job_of(a, L / NP / a.groups, L / NP % a.groups, L % NP * (D / NP), false), lds);
 }
 
-// Both chains of the backward pass in one launch: the states again, and the states' gradients.  Neither needs the other.
+// Both chains of the backward pass, the longer one first.  Neither needs the other.
 template <typename T, int D>
-__global__ __launch_bounds__(512, 1) void delta_backward_kernel(DeltaArgs a)
+__global__ __launch_bounds__((Shape<T, D, false>::THREADS), 1) void delta_backward_kernel(DeltaArgs a)
 {
-    __shared__ __attribute__((aligned(16))) ChainLds<T, D> lds;
-    const int total = a.B * a.H * (D / 16), blocks = (total + 7) / 8 * 8, which = blockIdx.x >= (unsigned)blocks;
-    const int L = chain_of(blockIdx.x - which * blocks, total), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) BothLds<T, D> lds;
+    constexpr int NP = PARTS<T, D>;
+    const int total = a.B * a.H * a.groups * NP, half = (total + 7) / 8 * 8;
+    const bool back = (int)blockIdx.x < half;
+    const int L = place_of(back ? blockIdx.x : blockIdx.x - half, total);
     if (L >= total) return;
-    const Place<T, D> p(a, L / (D / 16), L % (D / 16), wave & 3);
-    if (which) {
-        if (wave < 4) forward_chain<T, D, false>(a, p, lds);
-        else forward_helper<T, D, false>(a, p, lds);
-    } else {
-        if (wave < 4) backward_chain<T, D>(a, p, lds);
-        else backward_helper<T, D>(a, p, lds);
+    const Job j = job_of(a, L / NP / a.groups, L / NP % a.groups, L % NP * (D / NP), false);
+    if (back) run<T, D, true, KEEP>(a, j, lds.b);
+    else run<T, D, false, KEEP>(a, j, lds.f);
+}
+
+// B and M of the groups that another one follows, and for the backward pass B of the gradients (their map is M transposed).  The first
+// group needs no M.
+template <typename T, int D>
+__global__ __launch_bounds__((Shape<T, D, false>::THREADS), 1) void delta_sum_kernel(DeltaArgs a, int kinds)
+{
+    __shared__ __attribute__((aligned(16))) BothLds<T, D> lds;
+    constexpr int NP = PARTS<T, D>;
+    const int total = a.B * a.H * (a.groups - 1) * kinds * NP, L = place_of(blockIdx.x, total);
+    if (L >= total) return;
+    const int part = L % NP, kind = L / NP % kinds, g = L / NP / kinds % (a.groups - 1), bh = L / NP / kinds / (a.groups - 1);
+    if (kind == 1 && g == 0) return;
+    const Job j = job_of(a, bh, kind == 2 ? g + 1 : g, part * (D / NP), kind == 1);
+    if (kind == 2) run<T, D, true, SUM>(a, j, lds.b);
+    else run<T, D, false, SUM>(a, j, lds.f);
+}
+
+// The states that the groups start from: S <- M S + B from group to group (backward: M transposed, from the last).  A workgroup has 16 value
+// channels; S is in LDS, the products are fp32.
+template <int D>
+__global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int blocks)
+{
+    __shared__ float S[D][17];
+    const bool BACK = (int)blockIdx.x >= blocks;
+    const int bh = blockIdx.x % blocks / (D / 16), c0 = blockIdx.x % (D / 16) * 16;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, l4 = lane >> 4;
+    const float *in = BACK ? a.dstate_out : a.state_in;
+    for (int i = 0; i < a.groups; ++i) {
+        const int g = BACK ? a.groups - 1 - i : i;
+        const size_t at = ((size_t)bh * a.groups + g) * D * D;
+        float *start = (BACK ? a.gstart_b : a.gstart) + at;
+        if (i == 0) {
+            for (int e = tid; e < D * 16; e += 256) start[(size_t)(e / 16) * D + c0 + e % 16] = in ? in[((size_t)bh * D + e / 16) * D + c0 + e % 16] : 0.f;
+            continue;
+        }
+        const size_t before = BACK ? at + (size_t)D * D : at - (size_t)D * D;
+        const float *sum = (BACK ? a.gsum_b : a.gsum) + before, *map = a.gmap + before;
+        f32x4 c[D / 64];
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+            const int row = wave * (D / 4) + 16 * x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) c[x][r] = sum[(size_t)(row + 4 * l4 + r) * D + c0 + l16];
+            if (i > 1)
+                for (int k = 0; k < D; k += 4)
+                    c[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(BACK ? map[(size_t)(k + l4) * D + row + l16] : map[(size_t)(row + l16) * D + k + l4], S[k + l4][l16], c[x], 0, 0, 0);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = wave * (D / 4) + 16 * x + 4 * l4 + r;
+                S[row][l16] = c[x][r];
+                start[(size_t)row * D + c0 + l16] = c[x][r];
+            }
+        __syncthreads();
     }
+}
+
+// Groups: as many as shorten the passes.  One pass of all chunks without groups; with G groups one of a G-th for B and M, and one
+// of a G-th for the rest, each as often as its workgroups fill the chip's 256 compute units.
+int delta_groups(const DeltaArgs &a, bool backward)
+{
+    const int parts = a.D / (a.bf16 ? 64 : 32);
+    const long long one = (long long)a.B * a.H * parts * (backward ? 2 : 1);
+    auto rounds = [](long long wgs) { return (wgs + 255) / 256; };
+    const double alone = (double)a.chunks * rounds(one);
+    int best = 1;
+    double least = 0.8 * alone;                 // three short kernels for one long: not for little
+    for (int g = 2; g <= 32 && a.chunks / g >= 8; ++g) {
+        const double per = (a.chunks + g - 1) / g;
+        const double t = per * (rounds((long long)a.B * a.H * (g - 1) * parts * (backward ? 3 : 2)) + rounds(one * g)) + 4.0 * g;
+        if (t < least) { best = g; least = t; }
+    }
+    return best;
 }
 
 template <typename T, int D>
 static hipError_t chains(const DeltaArgs &a, bool backward, hipStream_t st)
 {
-    const int blocks = (a.B * a.H * (D / 16) + 7) / 8 * 8;
-    if (backward) launch_kernel((delta_backward_kernel<T, D>), dim3(2 * blocks), dim3(512), 0, st, a);
-    else launch_kernel((delta_forward_kernel<T, D>), dim3(blocks), dim3(512), 0, st, a);
+    const long long BH = (long long)a.B * a.H, total = (BH * a.groups * PARTS<T, D> + 7) / 8 * 8;
+    const dim3 threads(Shape<T, D, false>::THREADS);
+    if (a.groups > 1) {
+        const int kinds = backward ? 3 : 2, blocks = (int)BH * (D / 16);
+        launch_kernel((delta_sum_kernel<T, D>), dim3((unsigned)((BH * (a.groups - 1) * kinds * PARTS<T, D> + 7) / 8 * 8)), threads, 0, st, a, kinds);
+        launch_kernel((delta_start_kernel<D>), dim3(backward ? 2 * blocks : blocks), dim3(256), 0, st, a, blocks);
+    }
+    if (backward) launch_kernel((delta_backward_kernel<T, D>), dim3((unsigned)(2 * total)), threads, 0, st, a);
+    else launch_kernel((delta_forward_kernel<T, D>), dim3((unsigned)total), threads, 0, st, a);
     return take_launch_status();
 }
 
@@ -530,7 +498,7 @@ hipError_t launch_delta_chains(const DeltaArgs &a, bool backward, hipStream_t st
 
 hipError_t launch_delta_fwd(const DeltaArgs &a, hipStream_t st)
 {
-    if (const hipError_t e = launch_delta_chunk(a, st)) return e;
+    if (const hipError_t e = launch_delta_chunk(a, false, st)) return e;
     return launch_delta_chains(a, false, st);
 }
 

@@ -7,6 +7,7 @@
 // chunk to chunk in delta_chain.hip.  All exponents are differences of sums held in 64 bits; T keeps fp32 (three planes), P for bf16
 // tensors is rounded to bf16 (half a step of each term of O).
 #include <algorithm>
+#include <type_traits>
 
 #include "causal.h"
 #include "delta_planes.h"
@@ -14,24 +15,37 @@
 namespace salad {
 
 // ---- T and P ------------------------------------------------------------------------------------------------
-template <typename T, int D>
-__global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a)
+template <typename T, int D> struct ChunkLds {
+    static constexpr int P = planes_of<T>(), AP = 68;
+    float A[64][AP], Y[32][AP], X[64][AP];                      // A, a product on the way to its inverse, the inverse
+    u16 k[P][64][D + 8];
+    double bd[64];
+    float beta[64];
+};
+
+// BWD: the backward pass's operands
+template <typename T, int D, bool BWD>
+__global__ __launch_bounds__(256, 2) void delta_chunk_kernel(DeltaArgs a)
 {
-    constexpr int P = planes_of<T>(), NK = D / 32, AP = 68;
-    __shared__ double bd[64];
-    __shared__ float bt[64];
-    __shared__ __attribute__((aligned(16))) float A[64][AP], X[64][AP], Y[32][AP];     // A, its inverse, a product on the way
+    using L = ChunkLds<T, D>;
+    constexpr int P = L::P, NK = D / 32, AP = L::AP, KP = D + 8;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
+    L &lds = *reinterpret_cast<L *>(lds_bytes);
+    auto &A = lds.A; auto &X = lds.X; auto &Y = lds.Y; auto &bd = lds.bd;
     const int ch = blockIdx.x % a.chunks, bh = blockIdx.x / a.chunks, b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
     const int valid = min(delta_len(a, b) - ch * 64, 64);
     if (valid <= 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, l4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, l4 = lane >> 4;
     const size_t row0 = ((size_t)b * a.Hk + hk) * a.N + (size_t)ch * 64;
     const T *kp = reinterpret_cast<const T *>(a.k) + row0 * D, *qp = reinterpret_cast<const T *>(a.q) + row0 * D;
     const size_t at = (size_t)bh * a.chunks + ch;
+    Tile64<T, D> kt64;
+    kt64.load(kp, valid, tid);
     if (wave == 0) {
-        const size_t t = (size_t)bh * a.N + ch * 64 + lane;
-        float g = lane < valid ? a.g[t] : 0.f;
-        const float beta = lane < valid ? a.beta[t] : 0.f;
+        const size_t t = (size_t)bh * a.N + ch * 64 + min(lane, valid - 1);
+        float g = a.g[t], beta = a.beta[t];
+        g = lane < valid ? g : 0.f;
+        beta = lane < valid ? beta : 0.f;
         g = g < -100.f ? -100.f : g;                    // e^-100 is 0 in fp32 next to anything; -infinity would leave no differences
         double s = g;
 #pragma unroll
@@ -40,44 +54,53 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a)
             if (lane >= m) s += o;
         }
         const double last = __shfl(s, 63);
+        const float gamma = expf((float)s), tail = lane < valid ? expf((float)(last - s)) : 0.f, hi = (float)s;
         bd[lane] = s;
-        bt[lane] = beta;
+        lds.beta[lane] = beta;
         DeltaGate &gate = a.gate[at];
-        gate.gamma[lane] = expf((float)s);
-        gate.tail[lane] = lane < valid ? expf((float)(last - s)) : 0.f;
+        gate.gamma[lane] = gamma;
+        gate.tail[lane] = tail;
         gate.beta[lane] = beta;
-        const float hi = (float)s;
-        a.bsum[at * 64 + lane] = make_float2(hi, (float)(s - hi));
+        if (BWD) a.bsum[at * 64 + lane] = make_float2(hi, (float)(s - hi));
     }
+    const int tok = 16 * wave + l16;
+    Op<P> ownq[NK];
+    if (!BWD)
+#pragma unroll
+        for (int x = 0; x < NK; ++x) ownq[x] = frag_g(qp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, tok < valid);
+    kt64.store(&lds.k[0][0][0], tid);
+    __syncthreads();
     // A: rows 16 wave.., columns up to the diagonal.  P transposed, so that a lane has 4 neighbours of a row
     f32x4 kk[4], pp[4];
-    Op<P> own[NK], ownq[NK];
-    const int tok = 16 * wave + l16;
+    {
+        Op<P> own[NK];
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-        own[x] = frag_g(kp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, tok < valid);
-        if (a.pf) ownq[x] = frag_g(qp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, tok < valid);
+        for (int x = 0; x < NK; ++x) own[x] = frag_n<P>(&lds.k[0][0][0], 64 * KP, KP, 16 * wave, 32 * x, lane);
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) {
+            kk[ct] = pp[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (ct <= wave)
+#pragma unroll
+                for (int x = 0; x < NK; ++x) {
+                    const Op<P> f = frag_n<P>(&lds.k[0][0][0], 64 * KP, KP, 16 * ct, 32 * x, lane);
+                    mma(kk[ct], own[x], f);
+                    if (!BWD) mma(pp[ct], f, ownq[x]);
+                }
+        }
     }
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
-        kk[ct] = pp[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (ct <= wave)
-#pragma unroll
-            for (int x = 0; x < NK; ++x) {
-                const Op<P> f = frag_g(kp + (size_t)min(16 * ct + l16, valid - 1) * D + x * 32 + 8 * l4, 16 * ct + l16 < valid);
-                mma(kk[ct], own[x], f);
-                if (a.pf) mma(pp[ct], f, ownq[x]);
-            }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * wave + 4 * l4 + r, j = 16 * ct + l16;
-            A[i][j] = j < i ? bt[i] * expf((float)(bd[i] - bd[j])) * kk[ct][r] : 0.f;
+            A[i][j] = j < i ? lds.beta[i] * expf((float)(bd[i] - bd[j])) * kk[ct][r] : 0.f;
             X[i][j] = 0.f;
+            if (!BWD) {
+                const int l = 16 * ct + 4 * l4 + r;
+                pp[ct][r] = l <= tok ? a.scale * expf((float)(bd[tok] - bd[l])) * pp[ct][r] : 0.f;
+            }
         }
+    }
     __syncthreads();
     // inverses of the four 16 x 16 blocks on the diagonal, a wave each, a column a lane: x_i = [i = c] - sum_{j<i} A_ij x_j
     if (lane < 16) {
@@ -127,62 +150,44 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaArgs a)
         for (int r = 0; r < 4; ++r) X[32 + 16 * i + 4 * l4 + r][16 * j + l16] = -c[r];
     }
     __syncthreads();
-    // as operands: row tile = wave, halves kt of the contraction
-    u16 *tf = a.tf + at * DELTA_T_ELEMS, *ttf = a.ttf ? a.ttf + at * DELTA_T_ELEMS : nullptr;
+    // as operands: row tile = wave, the tokens of the contraction in the order of accumulators
+    auto out = [&](auto planes, u16 *to, int piece, const f32x4 &x, const f32x4 &y) {
+        constexpr int N = decltype(planes)::value;
+        const Op<N> o = op_of<N>(x, y);
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<bf16x8 *>(to + i * TRI + (piece * 64 + lane) * 8) = o.p[i];
+    };
+    const std::integral_constant<int, 3> three;
+    u16 *tf = a.tf + at * (3 * TRI);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-        const int row = 16 * wave + l16, k0 = 32 * kt + 8 * l4;
-        f32x4 x = *reinterpret_cast<const f32x4 *>(&X[row][k0]), y = *reinterpret_cast<const f32x4 *>(&X[row][k0 + 4]);
-        u32x2 p[3], q[3];
-        split4<3>(x, p);
-        split4<3>(y, q);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) *reinterpret_cast<u32x4 *>(tf + (((i * 4 + wave) * 2 + kt) * 64 + lane) * 8) = u32x4{p[i].x, p[i].y, q[i].x, q[i].y};
-        if (ttf) {
-            x = f32x4{X[k0][row], X[k0 + 1][row], X[k0 + 2][row], X[k0 + 3][row]};
-            y = f32x4{X[k0 + 4][row], X[k0 + 5][row], X[k0 + 6][row], X[k0 + 7][row]};
-            split4<3>(x, p);
-            split4<3>(y, q);
-#pragma unroll
-            for (int i = 0; i < 3; ++i) *reinterpret_cast<u32x4 *>(ttf + (((i * 4 + wave) * 2 + kt) * 64 + lane) * 8) = u32x4{p[i].x, p[i].y, q[i].x, q[i].y};
-        }
-    }
-    if (!a.pf) return;
-    // P through this wave's 16 rows of A, which nobody reads any more
-#pragma unroll
-    for (int ct = 0; ct < 4; ++ct) {
-        f32x4 c;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int j = 16 * ct + 4 * l4 + r;
-            c[r] = j <= tok ? a.scale * expf((float)(bd[tok] - bd[j])) * pp[ct][r] : 0.f;
-        }
-        *reinterpret_cast<f32x4 *>(&A[tok][16 * ct + 4 * l4]) = c;
-    }
-    __syncthreads();
-    u16 *pf = a.pf + at * (P * 4 * 2 * 64 * 8);
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-        const int k0 = 32 * kt + 8 * l4;
-        u32x2 p[P], q[P];
-        split4<P>(*reinterpret_cast<const f32x4 *>(&A[tok][k0]), p);
-        split4<P>(*reinterpret_cast<const f32x4 *>(&A[tok][k0 + 4]), q);
-#pragma unroll
-        for (int i = 0; i < P; ++i) *reinterpret_cast<u32x4 *>(pf + (((i * 4 + wave) * 2 + kt) * 64 + lane) * 8) = u32x4{p[i].x, p[i].y, q[i].x, q[i].y};
+        const int j = 32 * kt + 4 * l4;
+        if (kt == 0 || wave >= 2) out(three, tf, tri_lower(wave, kt), load4(&X[tok][j]), load4(&X[tok][j + 16]));
+        if (BWD && (kt == 1 || wave < 2))
+            out(three, a.ttf + at * (3 * TRI), tri_upper(wave, kt), f32x4{X[j][tok], X[j + 1][tok], X[j + 2][tok], X[j + 3][tok]},
+                f32x4{X[j + 16][tok], X[j + 17][tok], X[j + 18][tok], X[j + 19][tok]});
+        if (!BWD && (kt == 0 || wave >= 2))
+            out(std::integral_constant<int, P>(), a.pf + at * (P * TRI), tri_lower(wave, kt), pp[2 * kt], pp[2 * kt + 1]);
     }
 }
 
-hipError_t launch_delta_chunk(const DeltaArgs &a, hipStream_t st)
+template <typename T, int D, bool BWD>
+static hipError_t chunk(const DeltaArgs &a, hipStream_t st)
 {
-    const dim3 grid(a.B * a.H * a.chunks);
-    if (a.bf16) {
-        if (a.D == 128) launch_kernel((delta_chunk_kernel<u16, 128>), grid, dim3(256), 0, st, a);
-        else launch_kernel((delta_chunk_kernel<u16, 64>), grid, dim3(256), 0, st, a);
-    } else {
-        if (a.D == 128) launch_kernel((delta_chunk_kernel<float, 128>), grid, dim3(256), 0, st, a);
-        else launch_kernel((delta_chunk_kernel<float, 64>), grid, dim3(256), 0, st, a);
-    }
+    static bool done[16];
+    if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_chunk_kernel<T, D, BWD>), sizeof(ChunkLds<T, D>), done)) return e;
+    launch_kernel((delta_chunk_kernel<T, D, BWD>), dim3(a.B * a.H * a.chunks), dim3(256), sizeof(ChunkLds<T, D>), st, a);
     return take_launch_status();
+}
+
+hipError_t launch_delta_chunk(const DeltaArgs &a, bool backward, hipStream_t st)
+{
+    if (a.bf16) {
+        if (backward) return a.D == 128 ? chunk<u16, 128, true>(a, st) : chunk<u16, 64, true>(a, st);
+        return a.D == 128 ? chunk<u16, 128, false>(a, st) : chunk<u16, 64, false>(a, st);
+    }
+    if (backward) return a.D == 128 ? chunk<float, 128, true>(a, st) : chunk<float, 64, true>(a, st);
+    return a.D == 128 ? chunk<float, 128, false>(a, st) : chunk<float, 64, false>(a, st);
 }
 
 }  // namespace salad

@@ -86,7 +86,8 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, l4 = lane >> 4;
     const size_t at = (size_t)bh * a.chunks + ch, row0 = ((size_t)b * a.Hk + hk) * a.N + (size_t)ch * 64, vrow0 = (size_t)bh * a.N + (size_t)ch * 64;
     const T *qp = reinterpret_cast<const T *>(a.q) + row0 * D, *kp = reinterpret_cast<const T *>(a.k) + row0 * D;
-    const T *gp = reinterpret_cast<const T *>(a.dout) + vrow0 * D;
+    const T *gp = reinterpret_cast<const T *>(a.dout) + vrow0 * D, *vp = reinterpret_cast<const T *>(a.v) + vrow0 * D;
+    T *dvp = reinterpret_cast<T *>(a.dv) + vrow0 * D;
     const int tok = 16 * wave + l16;
     const bool live = tok < valid;
     f32x4 qs[NA], ks[NA], ke[NA], ru[4], ou[4];
@@ -94,7 +95,8 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     for (int x = 0; x < NA; ++x) qs[x] = ks[x] = ke[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 4; ++x) ru[x] = ou[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float sds = 0.f;                                                    // S_0 . dS
+    float sds = 0.f, rv = 0.f;                                          // S_0 . dS, dR . v
+    const float beta = a.gate[at].beta[tok];
     for (int cb = 0; cb < D / 32; ++cb) {
         const float *s0 = reinterpret_cast<const float *>(a.s0) + (at * D + cb * 32) * D, *s1 = a.ds1 + (at * D + cb * 32) * D;
         const float *up = reinterpret_cast<const float *>(a.u) + (at * D + cb * 32) * 64, *rp = a.dr + (at * D + cb * 32) * 64;
@@ -112,6 +114,21 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
         __syncthreads();
         const Op<P> go = frag_g(gp + (size_t)min(tok, valid - 1) * D + cb * 32 + 8 * l4, live);
         const Op<3> ui = frag_t<3>(Ut, UPL, UP, 16 * wave, 0, lane), ri = frag_t<3>(Rt, UPL, UP, 16 * wave, 0, lane);
+        {   // dv = beta dR: this lane's token and 8 value channels
+            const size_t at8 = (size_t)min(tok, valid - 1) * D + cb * 32 + 8 * l4;
+            const f32x4 va = load4(vp + at8), vb = load4(vp + at8 + 4);
+            f32x4 x, y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = (float)ri.p[0][i] + (float)ri.p[1][i] + (float)ri.p[2][i];
+                y[i] = (float)ri.p[0][i + 4] + (float)ri.p[1][i + 4] + (float)ri.p[2][i + 4];
+                rv += x[i] * va[i] + y[i] * vb[i];
+            }
+            if (live) {
+                store4(dvp + at8, x * beta);
+                store4(dvp + at8 + 4, y * beta);
+            }
+        }
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
             const Op<3> f0 = frag_t<3>(S0, SPL, SP, 16 * x, 0, lane);
@@ -127,7 +144,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
                 mma(ou[x], uj, go);
             }
     }
-    const float gamma = a.gate[at].gamma[tok], tail = a.gate[at].tail[tok], beta = a.gate[at].beta[tok];
+    const float gamma = a.gate[at].gamma[tok], tail = a.gate[at].tail[tok];
     const float2 bi = a.bsum[at * 64 + tok];
     Op<P> ki[NK], qi[NK];
 #pragma unroll
@@ -137,7 +154,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     }
     __syncthreads();                                                    // the blocks' tiles make room
     // pairs (i = own token, j): what A and P have to say
-    float rows = 0.f, db = 0.f;
+    float rows = 0.f, db = rv;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = kk, e = kk, dp = kk, cs = kk;
@@ -199,7 +216,6 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     if (lane == 0) red[wave] = end + gend * sds;
     if (l4 == 0) {
         fin[tok] = rows;
-        for (int s = 0; s < D / 16; ++s) db += a.dbv[(at * (D / 16) + s) * 64 + tok];
         if (live) a.dbeta[vrow0 + tok] = db;
     }
     Tile t;
@@ -300,7 +316,7 @@ hipError_t run(const DeltaArgs &a, hipStream_t st)
 
 hipError_t launch_delta_bwd(const DeltaArgs &a, hipStream_t st)
 {
-    if (const hipError_t e = launch_delta_chunk(a, st)) return e;
+    if (const hipError_t e = launch_delta_chunk(a, true, st)) return e;
     if (a.bf16) return a.D == 128 ? run<u16, 128>(a, st) : run<u16, 64>(a, st);
     return a.D == 128 ? run<float, 128>(a, st) : run<float, 64>(a, st);
 }

@@ -37,9 +37,11 @@ __device__ inline float high(uint32_t w) { return __uint_as_float(w & 0xffff0000
 // with that for the operands that are loaded a chunk ahead.
 __device__ inline void lds_barrier()
 {
+    __builtin_amdgcn_sched_barrier(0);      // what uses an operand late does not wait for it early
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // A store that the hardware drops where `offset` is not below the size that the resource was made with.  Loads and stores are counted
@@ -49,13 +51,13 @@ __device__ inline __amdgpu_buffer_rsrc_t bounded(T *p, int elems)
 {
     return __builtin_amdgcn_make_buffer_rsrc(p, 0, elems * (int)sizeof(T), 0x00027000);
 }
-__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, u16, int elem, float x)
+__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, u16, int elem, f32x4 x)
 {
-    __builtin_amdgcn_raw_buffer_store_b16((u16)pack2(x, 0.f), r, elem * 2, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}, r, elem * 2, 0, 0);
 }
-__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, float, int elem, float x)
+__device__ inline void store_bounded(__amdgpu_buffer_rsrc_t r, float, int elem, f32x4 x)
 {
-    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, elem * 4, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, elem * 4, 0, 0);
 }
 
 template <int P> struct Op { bf16x8 p[P]; };
@@ -141,6 +143,26 @@ __device__ inline Op<1> frag_g(const u16 *p, bool ok)
     w = ok ? w : u32x4{0, 0, 0, 0};
     return Op<1>{{__builtin_bit_cast(bf16x8, w)}};
 }
+// Accumulators as an operand.  The order of a contraction is free, so it is chosen such that two tiles of accumulators stand as the operand of
+// the next product as they are: lane group l4 of an operand over 32 indices has the four of the first tile and the four of the second.
+// Tokens: tile t has token 16 t + 4 l4 + r, so the operand goes 32 kt + 4 l4.., 32 kt + 16 + 4 l4.. .  Key channels: tiles 2 ks and
+// 2 ks + 1 are given the channels 32 ks + 8 l4 + r and 32 ks + 8 l4 + 4 + r, so that the operand's order is the channels' own.
+// Operand: row l % 16 of channel tile 2 ks + x, contraction over tokens 32 kt.. in that order, by transposing reads of a tile [64 tokens][D].
+template <int P>
+__device__ inline Op<P> frag_c(const u16 *tile, int plane, int pitch, int ks, int x, int kt, int lane)
+{
+    union { bf16x8 v; s16x4 h[2]; } u;
+    Op<P> f;
+    const u16 *at = tile + (32 * kt + 4 * (lane >> 4) + ((lane >> 2) & 3)) * pitch + 32 * ks + 8 * (lane & 3) + 4 * x;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane + 16 * pitch));
+        f.p[p] = u.v;
+    }
+    return f;
+}
+
 template <int P>
 __device__ inline Op<P> op_of(f32x4 x, f32x4 y)
 {
@@ -188,6 +210,9 @@ template <typename T, int D> struct Tile64 {
 // (tail and beta are zero for tokens that are not there)
 struct DeltaGate { float gamma[64], tail[64], beta[64]; };
 constexpr int DELTA_C = 64;
-constexpr size_t DELTA_T_ELEMS = 3 * 4 * 2 * 64 * 8;    // T of a chunk: planes, row tiles, halves of the contraction, lanes, 8 each
+// A chunk's triangular 64 x 64 matrix as operands: planes of six pieces (row tile, half of the contraction), 64 lanes x 8 elements each
+constexpr int TRI = 6 * 64 * 8;
+__host__ __device__ constexpr int tri_lower(int rt, int kt) { return rt < 2 ? rt : 2 * rt - 2 + kt; }         // (0,0) (1,0) (2,0) (2,1) (3,0) (3,1)
+__host__ __device__ constexpr int tri_upper(int rt, int kt) { return rt < 2 ? 2 * rt + kt : 2 + rt; }          // (0,0) (0,1) (1,0) (1,1) (2,1) (3,1)
 
 }  // namespace salad
