@@ -27,15 +27,15 @@ template <typename T, int D, bool BACK> struct Shape {
     static constexpr int P = planes_of<T>();
     static constexpr int SL = P == 1 ? 4 : 2;                               // waves of the chain, 16 value channels each
     static constexpr int KBUFS = P == 1 ? 2 : 1;                            // K (and Q) of two chunks, where LDS has room
-    static constexpr int KP = D + 8, VP = 16 * SL + 8, UO = P == 1 ? 1 : 3; // pitches; planes of u as a factor of O
+    static constexpr int VP = 16 * SL + 8, UO = P == 1 ? 1 : 3; // pitch; planes of u as a factor of O
     static constexpr bool QTILE = BACK || P == 1;                           // Q goes through LDS
     static constexpr int THREADS = 64 * (SL + 4);
 };
 
 template <typename T, int D, bool BACK> struct ChainLds {
     using H = Shape<T, D, BACK>;
-    u16 k[H::KBUFS][H::P * 64 * H::KP];
-    u16 q[BACK ? H::KBUFS : 1][H::QTILE ? H::P * 64 * H::KP : 8];
+    u16 k[H::KBUFS][H::P * 64 * D];
+    u16 q[BACK ? H::KBUFS : 1][H::QTILE ? H::P * 64 * D : 8];
     u16 t[3 * TRI];
     T v[64][H::VP];                             // values; backward: dO
     float gamma[64], tail[64], beta[64];
@@ -68,14 +68,16 @@ struct Job {
     bool unit;                                  // SUM: the chain from the unit matrix
 };
 
-__device__ inline f32x4 values(const u16 (*v)[72], int row, int c, int lane)    // rows row + 4 (lane / 16).., column c + lane % 16
+template <int VP>
+__device__ inline f32x4 values(const u16 (*v)[VP], int row, int c, int lane)    // rows row + 4 (lane / 16).., column c + lane % 16
 {
     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
         (s16x4 __attribute__((address_space(3))) *)LDS_PTR(&v[row + 4 * (lane >> 4) + ((lane >> 2) & 3)][c + 4 * (lane & 3)]));
     return f32x4{__uint_as_float((uint32_t)(u16)x[0] << 16), __uint_as_float((uint32_t)(u16)x[1] << 16), __uint_as_float((uint32_t)(u16)x[2] << 16),
                  __uint_as_float((uint32_t)(u16)x[3] << 16)};
 }
-__device__ inline f32x4 values(const float (*v)[40], int row, int c, int lane)
+template <int VP>
+__device__ inline f32x4 values(const float (*v)[VP], int row, int c, int lane)
 {
     f32x4 x;
 #pragma unroll
@@ -106,10 +108,10 @@ template <typename T, int D, bool BACK, Kind KIND>
 __device__ inline void chain(const DeltaArgs &a, const Job &j, ChainLds<T, D, BACK> &lds, int w, int lane)
 {
     using H = Shape<T, D, BACK>;
-    constexpr int P = H::P, NK = D / 32, KP = H::KP;
+    constexpr int P = H::P, NK = D / 32;
     const int l16 = lane & 15, l4 = lane >> 4, c = j.c0 + 16 * w + l16, n = j.end - j.first;
     const bool unit = KIND == SUM && !BACK && j.unit;       // the chain from the unit matrix, without values
-    f32x4 s[NK][2];
+    f32x4 s[2 * NK];                            // tile 2 ks + x
     // state: key channel 32 ks + 8 l4 + 4 x + r, value channel c
     const float *from = KIND == SUM ? nullptr : a.groups > 1 ? (BACK ? a.gstart_b : a.gstart) + ((size_t)j.bh * a.groups + j.group) * D * D
                                                              : BACK ? a.dstate_out + (a.dstate_out ? (size_t)j.bh * D * D : 0)
@@ -126,7 +128,7 @@ __device__ inline void chain(const DeltaArgs &a, const Job &j, ChainLds<T, D, BA
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 32 * ks + 8 * l4 + 4 * x + r;
-                s[ks][x][r] = unit ? (row == c ? 1.f : 0.f) : from ? from[(size_t)row * D + c] : 0.f;
+                s[2 * ks + x][r] = unit ? (row == c ? 1.f : 0.f) : from ? from[(size_t)row * D + c] : 0.f;
             }
     f32x4 x[4];                                 // backward: X = P^T dO of the next chunk
     auto load_x = [&](int i) __attribute__((always_inline)) {
@@ -134,87 +136,105 @@ __device__ inline void chain(const DeltaArgs &a, const Job &j, ChainLds<T, D, BA
         for (int rt = 0; rt < 4; ++rt) x[rt] = load4(a.dr + (((size_t)j.bh * a.chunks + j.end - 1 - i) * D + c) * 64 + 16 * rt + 4 * l4);
     };
     if (BACK && n > 0) load_x(0);
+    // What is an operand next is split while the matrix cores are at the product before: the tokens go in two halves, the first of them (of the
+    // last in the backward pass) complete one product earlier.
+    constexpr int A = BACK ? 2 : 0, B = BACK ? 0 : 2, KA = BACK ? 1 : 0, KB = BACK ? 0 : 1;      // first tiles of the halves; their contraction halves
+    Op<3> so[NK];                               // the state as an operand
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) so[ks] = op_of<3>(s[2 * ks], s[2 * ks + 1]);
     if (n > 0) lds_barrier();
     for (int i = 0; i < n; ++i) {
         const int ch = BACK ? j.end - 1 - i : j.first + i;
         const size_t at = (size_t)j.bh * a.chunks + ch;
         const u16 *K = lds.k[i & (H::KBUFS - 1)], *Q = lds.q[BACK ? i & (H::KBUFS - 1) : 0];
+        const float end = lds.gamma[63];
         if (KIND == KEEP)
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) store4((BACK ? a.ds1 : a.s0) + (at * D + c) * D + 32 * ks + 8 * l4 + 4 * y, s[ks][y]);
-        f32x4 acc[4];
+                for (int y = 0; y < 2; ++y) store4((BACK ? a.ds1 : a.s0) + (at * D + c) * D + 32 * ks + 8 * l4 + 4 * y, s[2 * ks + y]);
+        f32x4 acc[4], u[4];
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < 4; ++rt) acc[rt] = u[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // K S
+        auto k_s = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            const Op<3> so = op_of<3>(s[ks][0], s[ks][1]);
-            if constexpr (KIND == OUT)
-#pragma unroll
-                for (int p = 0; p < P; ++p) lds.side[i & 1].so[w][ks][p][lane] = __builtin_bit_cast(u32x4, so.p[p]);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) mma(acc[rt], frag_n<P>(K, 64 * KP, KP, 16 * rt, 32 * ks, lane), so);
-        }
-        // R, or dU
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            if (BACK) {
-                const f32x4 tail = load4(lds.tail + 16 * rt + 4 * l4);
-                acc[rt] = x[rt] + tail * acc[rt];
-            } else {
-                const f32x4 gamma = load4(lds.gamma + 16 * rt + 4 * l4), beta = load4(lds.beta + 16 * rt + 4 * l4);
-                if (unit) acc[rt] = -beta * gamma * acc[rt];
-                else acc[rt] = beta * (values(lds.v, 16 * rt, 16 * w, lane) - gamma * acc[rt]);
+            for (int ks = 0; ks < NK; ++ks) {
+                const Op<P> kf[2] = {frag_k<P, D>(K, 16 * half, ks, lane), frag_k<P, D>(K, 16 * half + 16, ks, lane)};
+                mmas<2>(acc + half, kf, so[ks]);
             }
-        }
-        if (BACK) load_x(min(i + 1, n - 1));
-        const Op<3> r0 = op_of<3>(acc[0], acc[1]), r1 = op_of<3>(acc[2], acc[3]);
-        f32x4 u[4];
+        };
+        // R, or dU, of a half, as an operand
+        auto r_op = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            u[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (BACK ? rt < 2 : true) mma(u[rt], tri_op(lds.t, BACK ? tri_upper(rt, 0) : tri_lower(rt, 0), lane), r0);
-            if (BACK ? true : rt >= 2) mma(u[rt], tri_op(lds.t, BACK ? tri_upper(rt, 1) : tri_lower(rt, 1), lane), r1);
-        }
-        if constexpr (KIND == OUT) {
-            const Op<H::UO> u0 = op_of<H::UO>(u[0], u[1]), u1 = op_of<H::UO>(u[2], u[3]);
-#pragma unroll
-            for (int p = 0; p < H::UO; ++p) {
-                lds.side[i & 1].uo[w][0][p][lane] = __builtin_bit_cast(u32x4, u0.p[p]);
-                lds.side[i & 1].uo[w][1][p][lane] = __builtin_bit_cast(u32x4, u1.p[p]);
+            for (int rt = half; rt < half + 2; ++rt) {
+                if (BACK) {
+                    acc[rt] = x[rt] + load4(lds.tail + 16 * rt + 4 * l4) * acc[rt];
+                } else {
+                    const f32x4 gamma = load4(lds.gamma + 16 * rt + 4 * l4), beta = load4(lds.beta + 16 * rt + 4 * l4);
+                    if (unit) acc[rt] = -beta * gamma * acc[rt];
+                    else acc[rt] = beta * (values(lds.v, 16 * rt, 16 * w, lane) - gamma * acc[rt]);
+                }
             }
-        }
-        if (KIND == KEEP)
+            return op_of<3>(acc[half], acc[half + 1]);
+        };
+        // u of a half on its way into the state, as an operand
+        auto u_op = [&](int half) __attribute__((always_inline)) {
+            if constexpr (KIND == OUT) {
+                const Op<H::UO> o = op_of<H::UO>(u[half], u[half + 1]);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) store4((BACK ? a.dr : a.u) + (at * D + c) * 64 + 16 * rt + 4 * l4, u[rt]);
-        Op<3> g0, g1;
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            if (BACK) {
-                const f32x4 gamma = load4(lds.gamma + 16 * rt + 4 * l4), beta = load4(lds.beta + 16 * rt + 4 * l4);
-                acc[rt] = a.scale * gamma * values(lds.v, 16 * rt, 16 * w, lane);
-                u[rt] *= -beta * gamma;
-            } else {
-                u[rt] *= load4(lds.tail + 16 * rt + 4 * l4);
+                for (int p = 0; p < H::UO; ++p) lds.side[i & 1].uo[w][half / 2][p][lane] = __builtin_bit_cast(u32x4, o.p[p]);
             }
+#pragma unroll
+            for (int rt = half; rt < half + 2; ++rt) {
+                if (KIND == KEEP) store4((BACK ? a.dr : a.u) + (at * D + c) * 64 + 16 * rt + 4 * l4, u[rt]);
+                if (BACK) u[rt] *= -load4(lds.gamma + 16 * rt + 4 * l4) * load4(lds.beta + 16 * rt + 4 * l4);
+                else u[rt] *= load4(lds.tail + 16 * rt + 4 * l4);
+            }
+            return op_of<3>(u[half], u[half + 1]);
+        };
+        // into the state, over half kt of the tokens
+        auto into = [&](const u16 *tile, int ks, int kt, const Op<3> &o) __attribute__((always_inline)) {
+            const Op<P> f[2] = {frag_c<P, D>(tile, ks, 0, kt, lane), frag_c<P, D>(tile, ks, 1, kt, lane)};
+            mmas<2>(s + 2 * ks, f, o);
+        };
+        if constexpr (KIND == OUT)
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                for (int p = 0; p < P; ++p) lds.side[i & 1].so[w][ks][p][lane] = __builtin_bit_cast(u32x4, so[ks].p[p]);
+        k_s(A);
+        Op<3> ta[4], tb[2];                     // T's pieces by the first half and by the second
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) ta[rt] = tri_op(lds.t, BACK ? tri_upper(rt, 1) : tri_lower(rt, 0), lane);
+        const Op<3> ra = r_op(A);
+        k_s(B);
+#pragma unroll
+        for (int x2 = 0; x2 < 2 * NK; ++x2) s[x2] *= end;
+        mmas<4>(u, ta, ra);
+        const Op<3> rb = r_op(B);
+        tb[0] = tri_op(lds.t, BACK ? tri_upper(0, 0) : tri_lower(2, 1), lane);
+        tb[1] = tri_op(lds.t, BACK ? tri_upper(1, 0) : tri_lower(3, 1), lane);
+        if (BACK) {
+            load_x(min(i + 1, n - 1));
+            f32x4 go[4];
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) go[rt] = a.scale * load4(lds.gamma + 16 * rt + 4 * l4) * values(lds.v, 16 * rt, 16 * w, lane);
+            const Op<3> g0 = op_of<3>(go[0], go[1]), g1 = op_of<3>(go[2], go[3]);
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) { into(Q, ks, 0, g0); into(Q, ks, 1, g1); }
         }
-        if (BACK) { g0 = op_of<3>(acc[0], acc[1]); g1 = op_of<3>(acc[2], acc[3]); }
-        const Op<3> u0 = op_of<3>(u[0], u[1]), u1 = op_of<3>(u[2], u[3]);
-        const float end = lds.gamma[63];
+        mmas<2>(u + B, tb, rb);
+        const Op<3> ua = u_op(A);
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) into(K, ks, KA, ua);
+        const Op<3> ub = u_op(B);
         lds_barrier();
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                s[ks][y] *= end;
-                if (BACK) {
-                    mma(s[ks][y], frag_c<P>(Q, 64 * KP, KP, ks, y, 0, lane), g0);
-                    mma(s[ks][y], frag_c<P>(Q, 64 * KP, KP, ks, y, 1, lane), g1);
-                }
-                mma(s[ks][y], frag_c<P>(K, 64 * KP, KP, ks, y, 0, lane), u0);
-                mma(s[ks][y], frag_c<P>(K, 64 * KP, KP, ks, y, 1, lane), u1);
-            }
+        for (int ks = 0; ks < NK; ++ks) {
+            into(K, ks, KB, ub);
+            so[ks] = op_of<3>(s[2 * ks], s[2 * ks + 1]);
+        }
         if (H::KBUFS == 1) lds_barrier();
         lds_barrier();
     }
@@ -228,7 +248,7 @@ __device__ inline void chain(const DeltaArgs &a, const Job &j, ChainLds<T, D, BA
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) to[(size_t)(32 * ks + 8 * l4 + 4 * x + r) * D + c] = s[ks][x][r];
+                for (int r = 0; r < 4; ++r) to[(size_t)(32 * ks + 8 * l4 + 4 * x + r) * D + c] = s[2 * ks + x][r];
 }
 
 // The next chunk's operands, and O of the chunk before.  Wave w of 4: 16 tokens of O.
@@ -236,7 +256,7 @@ template <typename T, int D, bool BACK, Kind KIND>
 __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, BACK> &lds, int w, int lane)
 {
     using H = Shape<T, D, BACK>;
-    constexpr int P = H::P, NK = D / 32, KP = H::KP, SL = H::SL;
+    constexpr int P = H::P, NK = D / 32, SL = H::SL;
     const int t = w * 64 + lane, l16 = lane & 15, l4 = lane >> 4, n = j.end - j.first;
     if (n <= 0) return;
     const int b = j.bh / a.H, h = j.bh - b * a.H, hk = h / (a.H / a.Hk);
@@ -254,8 +274,8 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
     auto load = [&](int i) __attribute__((always_inline)) {
         const int ch = chunk_of(i), valid = valid_of(ch);
         const size_t at = (size_t)j.bh * a.chunks + ch;
-        kr.load(k + (size_t)ch * 64 * D, valid, t);
-        if (BACK) qr.load(q + (size_t)ch * 64 * D, valid, t);
+        kr.load_clamped(k + (size_t)ch * 64 * D, valid - 1, t);
+        if (BACK) qr.load_clamped(q + (size_t)ch * 64 * D, valid - 1, t);
         vr.load(v + (size_t)ch * 64 * D, valid - 1, t);
 #pragma unroll
         for (int x = 0; x < NT; ++x) tr[x] = *reinterpret_cast<const u32x4 *>(tri + at * (3 * TRI) + (size_t)min(x * 256 + t, 3 * TRI / 8 - 1) * 8);
@@ -271,8 +291,8 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
         else if (t < 192) lds.beta[t - 128] = gr;
     };
     auto put_rows = [&](int i) __attribute__((always_inline)) {
-        kr.store(lds.k[i & (H::KBUFS - 1)], t);
-        if (BACK) qr.store(lds.q[i & (H::KBUFS - 1)], t);
+        kr.store_swizzled(lds.k[i & (H::KBUFS - 1)], t);
+        if (BACK) qr.store_swizzled(lds.q[i & (H::KBUFS - 1)], t);
     };
     // O: what it takes besides the chain's operands, loaded in its chunk, used in the next
     Op<P> pf[2], qn[P == 1 ? 1 : NK];
@@ -286,7 +306,7 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
             for (int p = 0; p < P; ++p)
                 pf[kt].p[p] = *reinterpret_cast<const bf16x8 *>(a.pf + at * (P * TRI) + p * TRI + (tri_lower(w, w < 2 ? 0 : kt) * 64 + lane) * 8);
         gamma = a.scale * a.gate[at].gamma[16 * w + l16];
-        if constexpr (H::QTILE) qr.load(q + (size_t)ch * 64 * D, valid, t);
+        if constexpr (H::QTILE) qr.load_clamped(q + (size_t)ch * 64 * D, valid - 1, t);
         else
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) qn[ks] = frag_g(q + (size_t)(ch * 64 + min(16 * w + l16, valid - 1)) * D + 32 * ks + 8 * l4, true);
@@ -299,7 +319,7 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
             Op<P> qo[NK];
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) {
-                if constexpr (H::QTILE) qo[ks] = frag_n<P>(lds.q[0], 64 * KP, KP, 16 * w, 32 * ks, lane);
+                if constexpr (H::QTILE) qo[ks] = frag_k<P, D>(lds.q[0], 16 * w, ks, lane);
                 else qo[ks] = qn[ks];
             }
 #pragma unroll
@@ -337,7 +357,7 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
         if (H::KBUFS > 1) put_rows(i + 1);
         lds_barrier();
         put_small(min(i + 1, n - 1));
-        if (KIND == OUT && H::QTILE) qr.store(lds.q[0], t);
+        if (KIND == OUT && H::QTILE) qr.store_swizzled(lds.q[0], t);
         if (H::KBUFS == 1) { lds_barrier(); put_rows(i + 1); }
         lds_barrier();
     }

@@ -73,6 +73,19 @@ __device__ inline void mma(f32x4 &c, const Op<PA> &a, const Op<PB> &b)
             if (s - i >= 0 && s - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], c, 0, 0, 0);
 }
 
+// N such products by the same B in turn: a product takes longer than the next one's issue, so neighbours go to different accumulators
+template <int N, int PA, int PB>
+__device__ inline void mmas(f32x4 *c, const Op<PA> *a, const Op<PB> &b)
+{
+#pragma unroll
+    for (int s = 2; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (s - i >= 0 && s - i < PB)
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n].p[i], b.p[s - i], c[n], 0, 0, 0);
+}
+
 // four floats as P planes
 template <int P>
 __device__ inline void split4(f32x4 x, u32x2 (&o)[P])
@@ -147,17 +160,32 @@ __device__ inline Op<1> frag_g(const u16 *p, bool ok)
 // the next product as they are: lane group l4 of an operand over 32 indices has the four of the first tile and the four of the second.
 // Tokens: tile t has token 16 t + 4 l4 + r, so the operand goes 32 kt + 4 l4.., 32 kt + 16 + 4 l4.. .  Key channels: tiles 2 ks and
 // 2 ks + 1 are given the channels 32 ks + 8 l4 + r and 32 ks + 8 l4 + 4 + r, so that the operand's order is the channels' own.
-// Operand: row l % 16 of channel tile 2 ks + x, contraction over tokens 32 kt.. in that order, by transposing reads of a tile [64 tokens][D].
-template <int P>
-__device__ inline Op<P> frag_c(const u16 *tile, int plane, int pitch, int ks, int x, int kt, int lane)
+//
+// A tile [64 tokens][D] that is read both ways, along its rows (row r0 + l % 16, channels 32 ks.. in their order) and down its columns (row l % 16
+// of channel tile 2 ks + x, tokens 32 kt.. in the accumulators' order, by transposing reads).  Its rows' 16-byte pieces are
+// swizzled, so that 16 rows of one piece and 4 rows of 4 pieces both spread over the banks.
+template <int D> __device__ inline int sigma(int r) { return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3); }
+template <int P, int D>
+__device__ inline Op<P> frag_k(const u16 *tile, int r0, int ks, int lane)
+{
+    Op<P> f;
+    const int row = r0 + (lane & 15);
+    const u16 *at = tile + row * D + (((4 * ks + (lane >> 4)) ^ sigma<D>(row)) << 3);
+#pragma unroll
+    for (int p = 0; p < P; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(at + p * 64 * D);
+    return f;
+}
+template <int P, int D>
+__device__ inline Op<P> frag_c(const u16 *tile, int ks, int x, int kt, int lane)
 {
     union { bf16x8 v; s16x4 h[2]; } u;
     Op<P> f;
-    const u16 *at = tile + (32 * kt + 4 * (lane >> 4) + ((lane >> 2) & 3)) * pitch + 32 * ks + 8 * (lane & 3) + 4 * x;
+    const int row = 32 * kt + 4 * (lane >> 4) + ((lane >> 2) & 3);          // and 16 rows on, swizzled alike
+    const u16 *at = tile + row * D + (((4 * ks + (lane & 3)) ^ sigma<D>(row)) << 3) + 4 * x;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane));
-        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * plane + 16 * pitch));
+        u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * 64 * D));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)LDS_PTR(at + p * 64 * D + 16 * D));
         f.p[p] = u.v;
     }
     return f;
@@ -193,6 +221,11 @@ template <typename T, int D> struct Tile64 {
             r[i] = row < valid ? w : u32x4{0, 0, 0, 0};
         }
     }
+    __device__ inline void load_clamped(const T *base, int last, int tid)       // rows behind the last are the last once more
+    {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) r[i] = *reinterpret_cast<const u32x4 *>(base + (unsigned)(min(i * RPP + tid / LPR, last) * D + tid % LPR * PER));
+    }
     __device__ inline void store(u16 *tile, int tid) const
     {
 #pragma unroll
@@ -200,6 +233,16 @@ template <typename T, int D> struct Tile64 {
             u16 *at = tile + (i * RPP + tid / LPR) * PITCH + tid % LPR * PER;
             if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x4 *>(at) = r[i];
             else put4<3>(at, PLANE, __builtin_bit_cast(f32x4, r[i]));
+        }
+    }
+    __device__ inline void store_swizzled(u16 *tile, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int row = i * RPP + tid / LPR, col = tid % LPR * PER;
+            u16 *at = tile + row * D + (((col >> 3) ^ sigma<D>(row)) << 3) + (col & 7);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x4 *>(at) = r[i];
+            else put4<3>(at, 64 * D, __builtin_bit_cast(f32x4, r[i]));
         }
     }
 };
