@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import subprocess
 from typing import Optional, Sequence, Tuple
 
@@ -174,15 +175,15 @@ def lib() -> C.CDLL:
         L.salad_timing_read.restype = C.c_int
         L.salad_timing_read.argtypes = [C.POINTER(KernelTimes), C.c_int32]
         L.salad_window_attn_workspace_bytes.restype = C.c_size_t
-        L.salad_window_attn_workspace_bytes.argtypes = [C.POINTER(WindowParams), C.c_int32]
+        L.salad_window_attn_workspace_bytes.argtypes = [C.c_void_p, C.c_int32]
         for f in (L.salad_window_attn_fwd, L.salad_window_attn_bwd):
-            f.restype, f.argtypes = C.c_int, [C.POINTER(WindowParams)]
+            f.restype, f.argtypes = C.c_int, [C.c_void_p]
         L.salad_window_cache_append.restype = C.c_int
         L.salad_window_cache_append.argtypes = [C.c_void_p] * 4 + [C.c_int32] * 8 + [C.c_void_p] * 3
         L.salad_gated_delta_workspace_bytes.restype = C.c_size_t
-        L.salad_gated_delta_workspace_bytes.argtypes = [C.POINTER(DeltaParams), C.c_int32]
+        L.salad_gated_delta_workspace_bytes.argtypes = [C.c_void_p, C.c_int32]
         for f in (L.salad_gated_delta_fwd, L.salad_gated_delta_bwd):
-            f.restype, f.argtypes = C.c_int, [C.POINTER(DeltaParams)]
+            f.restype, f.argtypes = C.c_int, [C.c_void_p]
         L.salad_tune.restype = C.c_int
         L.salad_tune.argtypes = [C.c_char_p, C.c_int32]
         _lib = L
@@ -446,7 +447,7 @@ class CausalWorkspace:
     long as the graph.  Calls that may overlap must not share one."""
 
     def __init__(self, nbytes: int = 0, device=None):
-        self.buf, self.kept, self.ptr, self.bytes = None, [], None, 0
+        self.buf, self.kept, self.ptr, self.bytes = None, [], 0, 0
         if nbytes:
             import torch
             self._grow(int(nbytes), torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device))
@@ -469,69 +470,79 @@ class CausalWorkspace:
         return self.ptr, self.bytes
 
 
-def _call_on(device, call):
-    """Runs call() with `device` current: launches go to it and to its current stream, whatever device the thread is on."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        return call()
-    with torch.cuda.device(device):
-        return call()
+# The parameter structures are packed in one go: filled field by field they take longer than a token's kernels.
+_pack_window = struct.Struct("@10if12PNP").pack
+_pack_delta = struct.Struct("@6if18PNP").pack
 
 
-def _tensor(name, t, shape, dtype, device, optional=False):
-    """Checks a tensor argument; its pointer, or None."""
+def _tensor(name, t, shape, dtype, index, optional=False) -> int:
+    """Checks a tensor argument (device: cuda:`index`); its pointer, or 0."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return t.data_ptr()
     if t is None:
         if optional:
-            return None
+            return 0
         raise ValueError(f"{name} is missing")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
-    return t.data_ptr()
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    raise ValueError(f"{name} is not contiguous")
 
 
-def _query(q):
-    if q.dim() != 4:
-        raise ValueError(f"q has {q.dim()} dimensions, expected [B, H, N, d]")
+def _rows(name, t, letters):
+    if t.dim() != 4:
+        raise ValueError(f"{name} has {t.dim()} dimensions, expected {letters}")
+    return t.shape
+
+
+def _device(q) -> int:
     if not q.is_cuda:
         raise ValueError("q is not on a GPU: there is no CPU path")
-    return _dtype_code(q)
+    return q.get_device()
 
 
-def _window_params(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale):
+def _run(index, make, fn, need, backward, workspace):
+    """make() -> (arguments of the packing up to the workspace, result), with the tensors' device current: what it allocates and the launch go
+    there, whatever device the thread is on, and to that device's current stream."""
     import torch
-    p = WindowParams()
-    p.dtype = _query(q)
-    B, H, Nq, d = q.shape
-    if k.dim() != 4:
-        raise ValueError(f"k has {k.dim()} dimensions, expected [B, Hk, Nk, d]")
-    Hk, Nk = k.shape[1], k.shape[2]
-    p.B, p.H, p.Hk, p.Nq, p.Nk, p.d = B, H, Hk, Nq, Nk, d
-    p.window, p.sinks, p.ring, p.softmax_scale = int(window), int(sinks), int(bool(ring)), softmax_scale
-    p.q = _tensor("q", q, q.shape, q.dtype, q.device)
-    p.k = _tensor("k", k, (B, Hk, Nk, d), q.dtype, q.device)
-    p.v = _tensor("v", v, (B, Hk, Nk, d), q.dtype, q.device)
-    p.q_lens = _tensor("q_lens", q_lens, (B,), torch.int32, q.device, optional=True)
-    p.kv_lens = _tensor("kv_lens", kv_lens, (B,), torch.int32, q.device, optional=True)
-    return p
-
-
-def _with_workspace(p, need: int, workspace, device):
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _run(index, make, fn, need, backward, workspace)
+    pack, args, result = make()
+    stream = _stream()
     ws = workspace
-    if need:
-        ws = CausalWorkspace() if workspace is None else workspace
-        if workspace is None:
-            import torch
-            ws.buf = torch.empty(need + 256, dtype=torch.uint8, device=device)      # one call's own, also under capture
-            ws.ptr, ws.bytes = (ws.buf.data_ptr() + 255) & ~255, need
-        p.workspace, p.workspace_bytes = ws.room(need, device)
-    p.hip_stream = _stream()
-    return ws
+    if ws is None or ws.buf is None or ws.buf.get_device() != index:
+        # sized first: one call's own scratch (also under capture), or the first call of a workspace
+        nbytes = int(need(pack(*args, 0, 0, stream), backward))
+        if ws is not None:
+            ptr, have = ws.room(nbytes, torch.device("cuda", index))
+        elif nbytes:
+            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=torch.device("cuda", index))
+            ptr, have = (buf.data_ptr() + 255) & ~255, nbytes
+        else:
+            ptr, have = 0, 0
+    else:
+        ptr, have = ws.ptr, ws.bytes
+    st = fn(pack(*args, ptr, have, stream))
+    if st == SALAD_ENOSPC and ws is not None:
+        ptr, have = ws.room(int(need(pack(*args, 0, 0, stream), backward)), torch.device("cuda", index))
+        st = fn(pack(*args, ptr, have, stream))
+    _check(st)
+    return result
+
+
+def _window_args(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale):
+    import torch
+    B, H, Nq, d = _rows("q", q, "[B, H, Nq, d]")
+    _, Hk, Nk, _ = _rows("k", k, "[B, Hk, Nk, d]")
+    index, dt = _device(q), q.dtype
+    kv = (B, Hk, Nk, d)
+    return index, (B, H, Hk, Nq, Nk, d, _dtype_code(q), int(window), int(sinks), 1 if ring else 0, softmax_scale,
+                   _tensor("q", q, q.shape, dt, index), _tensor("k", k, kv, dt, index), _tensor("v", v, kv, dt, index)), (
+                       _tensor("q_lens", q_lens, (B,), torch.int32, index, True), _tensor("kv_lens", kv_lens, (B,), torch.int32, index, True))
 
 
 def salad_window_attn_fwd(q, k, v, window: int, sinks: int = 0, *, q_lens=None, kv_lens=None, ring: bool = False, softmax_scale: float = 0.0,
@@ -540,70 +551,58 @@ def salad_window_attn_fwd(q, k, v, window: int, sinks: int = 0, *, q_lens=None, 
     Pass `lse` (fp32 [B,H,Nq]) to have the rows' log-sum-exp, which the backward call takes.  See include/salad.h for positions,
     lengths and the rolling cache (`ring`)."""
     import torch
-    p = _window_params(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale)
+    index, head, lens = _window_args(q, k, v, window, sinks, q_lens, kv_lens, ring, softmax_scale)
 
-    def call():
+    def make():
         o = torch.empty_like(q) if out is None else out
-        p.out = _tensor("out", o, q.shape, q.dtype, q.device)
-        p.lse = _tensor("lse", lse, q.shape[:3], torch.float32, q.device, optional=True)
-        keep = _with_workspace(p, int(lib().salad_window_attn_workspace_bytes(C.byref(p), 0)), workspace, q.device)
-        _check(lib().salad_window_attn_fwd(C.byref(p)))
-        del keep
-        return o
-    return _call_on(q.device, call)
+        return _pack_window, (*head, _tensor("out", o, q.shape, q.dtype, index), _tensor("lse", lse, q.shape[:3], torch.float32, index, True),
+                              *lens, 0, 0, 0, 0), o
+    L = lib()
+    return _run(index, make, L.salad_window_attn_fwd, L.salad_window_attn_workspace_bytes, 0, workspace)
 
 
 def salad_window_attn_bwd(q, k, v, out, lse, dout, window: int, sinks: int = 0, *, q_lens=None, kv_lens=None, softmax_scale: float = 0.0,
                           dq=None, dk=None, dv=None, workspace: Optional[CausalWorkspace] = None):
     """Gradients (dq, dk, dv) of sum(out * dout) for salad_window_attn_fwd with the same arguments; out and lse are that call's."""
     import torch
-    p = _window_params(q, k, v, window, sinks, q_lens, kv_lens, False, softmax_scale)
+    index, head, lens = _window_args(q, k, v, window, sinks, q_lens, kv_lens, False, softmax_scale)
 
-    def call():
-        p.out = _tensor("out", out, q.shape, q.dtype, q.device)
-        p.lse = _tensor("lse", lse, q.shape[:3], torch.float32, q.device)
-        p.dout = _tensor("dout", dout, q.shape, q.dtype, q.device)
-        g = [torch.empty_like(x) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv))]
-        p.dq, p.dk, p.dv = (_tensor(n, x, y.shape, q.dtype, q.device) for n, x, y in zip(("dq", "dk", "dv"), g, (q, k, v)))
-        keep = _with_workspace(p, int(lib().salad_window_attn_workspace_bytes(C.byref(p), 1)), workspace, q.device)
-        _check(lib().salad_window_attn_bwd(C.byref(p)))
-        del keep
-        return tuple(g)
-    return _call_on(q.device, call)
+    def make():
+        g = tuple(torch.empty_like(x) if y is None else y for x, y in ((q, dq), (k, dk), (v, dv)))
+        return _pack_window, (*head, _tensor("out", out, q.shape, q.dtype, index), _tensor("lse", lse, q.shape[:3], torch.float32, index), *lens,
+                              _tensor("dout", dout, q.shape, q.dtype, index),
+                              *(_tensor(n, x, y.shape, q.dtype, index) for n, x, y in zip(("dq", "dk", "dv"), g, (q, k, v)))), g
+    L = lib()
+    return _run(index, make, L.salad_window_attn_bwd, L.salad_window_attn_workspace_bytes, 1, workspace)
 
 
 def salad_window_cache_append(k_new, v_new, k_cache, v_cache, sinks: int, kv_lens, *, q_lens=None, ring: bool = True) -> None:
     """New tokens [B,Hk,Nq,d] into the rows of their positions in a cache [B,Hk,Nk,d]; kv_lens (device int32 [B]) is the length with them,
     as the attention call behind takes it."""
     import torch
-    code = _query(k_new)
-    B, Hk, Nq, d = k_new.shape
-    if k_cache.dim() != 4:
-        raise ValueError(f"k_cache has {k_cache.dim()} dimensions, expected [B, Hk, Nk, d]")
-    Nk, dev, dt = k_cache.shape[2], k_new.device, k_new.dtype
-    ptrs = [_tensor("k_new", k_new, k_new.shape, dt, dev), _tensor("v_new", v_new, k_new.shape, dt, dev),
-            _tensor("k_cache", k_cache, (B, Hk, Nk, d), dt, dev), _tensor("v_cache", v_cache, (B, Hk, Nk, d), dt, dev)]
-    lens = [_tensor("q_lens", q_lens, (B,), torch.int32, dev, optional=True), _tensor("kv_lens", kv_lens, (B,), torch.int32, dev)]
-    _call_on(dev, lambda: _check(lib().salad_window_cache_append(*ptrs, B, Hk, Nq, Nk, d, code, int(sinks), int(bool(ring)), *lens, _stream())))
+    B, Hk, Nq, d = _rows("k_new", k_new, "[B, Hk, Nq, d]")
+    Nk, dt, index = _rows("k_cache", k_cache, "[B, Hk, Nk, d]")[2], k_new.dtype, _device(k_new)
+    cache = (B, Hk, Nk, d)
+    args = (_tensor("k_new", k_new, k_new.shape, dt, index), _tensor("v_new", v_new, k_new.shape, dt, index),
+            _tensor("k_cache", k_cache, cache, dt, index), _tensor("v_cache", v_cache, cache, dt, index), B, Hk, Nq, Nk, d, _dtype_code(k_new),
+            int(sinks), 1 if ring else 0, _tensor("q_lens", q_lens, (B,), torch.int32, index, True) or None,
+            _tensor("kv_lens", kv_lens, (B,), torch.int32, index))
+    if index == torch.cuda.current_device():
+        _check(lib().salad_window_cache_append(*args, _stream()))
+    else:
+        with torch.cuda.device(index):
+            _check(lib().salad_window_cache_append(*args, _stream()))
 
 
-def _delta_params(q, k, v, g, beta, state, lens, scale):
+def _delta_args(q, k, v, g, beta, state, lens, scale):
     import torch
-    p = DeltaParams()
-    p.dtype = _query(q)
-    B, Hk, N, d = q.shape
-    if v.dim() != 4:
-        raise ValueError(f"v has {v.dim()} dimensions, expected [B, H, N, d]")
-    H, dev = v.shape[1], q.device
-    p.B, p.H, p.Hk, p.N, p.d, p.scale = B, H, Hk, N, d, scale
-    p.q = _tensor("q", q, q.shape, q.dtype, dev)
-    p.k = _tensor("k", k, q.shape, q.dtype, dev)
-    p.v = _tensor("v", v, (B, H, N, d), q.dtype, dev)
-    p.g = _tensor("g", g, (B, H, N), torch.float32, dev)
-    p.beta = _tensor("beta", beta, (B, H, N), torch.float32, dev)
-    p.state_in = _tensor("state", state, (B, H, d, d), torch.float32, dev, optional=True)
-    p.lens = _tensor("lens", lens, (B,), torch.int32, dev, optional=True)
-    return p
+    B, Hk, N, d = _rows("q", q, "[B, Hk, N, d]")
+    H = _rows("v", v, "[B, H, N, d]")[1]
+    index, dt = _device(q), q.dtype
+    return index, (B, H, Hk, N, d, _dtype_code(q), scale, _tensor("q", q, q.shape, dt, index), _tensor("k", k, q.shape, dt, index),
+                   _tensor("v", v, (B, H, N, d), dt, index), _tensor("g", g, (B, H, N), torch.float32, index),
+                   _tensor("beta", beta, (B, H, N), torch.float32, index)), _tensor("state", state, (B, H, d, d), torch.float32, index, True), (
+                       _tensor("lens", lens, (B,), torch.int32, index, True))
 
 
 def salad_gated_delta_fwd(q, k, v, g, beta, *, state=None, state_out=None, lens=None, scale: float = 0.0, out=None,
@@ -611,18 +610,16 @@ def salad_gated_delta_fwd(q, k, v, g, beta, *, state=None, state_out=None, lens=
     """The gated delta rule over the tokens of a call, any number: q, k [B,Hk,N,d], v [B,H,N,d], g and beta fp32 [B,H,N] and a
     state fp32 [B,H,d,d] (None: zeros) -> (out [B,H,N,d], the state after the last token).  `state_out` may be `state` itself."""
     import torch
-    p = _delta_params(q, k, v, g, beta, state, lens, scale)
+    index, head, s_in, ln = _delta_args(q, k, v, g, beta, state, lens, scale)
 
-    def call():
+    def make():
         o = torch.empty_like(v) if out is None else out
-        s = torch.empty(p.B, p.H, p.d, p.d, dtype=torch.float32, device=q.device) if state_out is None else state_out
-        p.out = _tensor("out", o, v.shape, q.dtype, q.device)
-        p.state_out = _tensor("state_out", s, (p.B, p.H, p.d, p.d), torch.float32, q.device)
-        keep = _with_workspace(p, int(lib().salad_gated_delta_workspace_bytes(C.byref(p), 0)), workspace, q.device)
-        _check(lib().salad_gated_delta_fwd(C.byref(p)))
-        del keep
-        return o, s
-    return _call_on(q.device, call)
+        shape = (v.shape[0], v.shape[1], v.shape[3], v.shape[3])
+        s = torch.empty(shape, dtype=torch.float32, device=q.device) if state_out is None else state_out
+        return _pack_delta, (*head, _tensor("out", o, v.shape, q.dtype, index), s_in, _tensor("state_out", s, shape, torch.float32, index), ln,
+                             0, 0, 0, 0, 0, 0, 0, 0), (o, s)
+    L = lib()
+    return _run(index, make, L.salad_gated_delta_fwd, L.salad_gated_delta_workspace_bytes, 0, workspace)
 
 
 def salad_gated_delta_bwd(q, k, v, g, beta, dout, *, state=None, dstate_out=None, lens=None, scale: float = 0.0, dq=None, dk=None, dv=None,
@@ -630,20 +627,16 @@ def salad_gated_delta_bwd(q, k, v, g, beta, dout, *, state=None, dstate_out=None
     """Gradients (dq, dk, dv, dg, dbeta, dstate) of sum(out * dout) + sum(state_out * dstate_out) for salad_gated_delta_fwd with the same
     inputs; dstate is the gradient of the state before the first token."""
     import torch
-    p = _delta_params(q, k, v, g, beta, state, lens, scale)
+    index, head, s_in, ln = _delta_args(q, k, v, g, beta, state, lens, scale)
 
-    def call():
-        p.dout = _tensor("dout", dout, v.shape, q.dtype, q.device)
-        p.dstate_out = _tensor("dstate_out", dstate_out, (p.B, p.H, p.d, p.d), torch.float32, q.device, optional=True)
-        grads = []
-        for n, given, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v), ("dg", dg, g), ("dbeta", dbeta, beta)):
-            x = torch.empty_like(like) if given is None else given
-            setattr(p, n, _tensor(n, x, like.shape, like.dtype, q.device))
-            grads.append(x)
-        s = torch.empty(p.B, p.H, p.d, p.d, dtype=torch.float32, device=q.device) if dstate is None else dstate
-        p.dstate_in = _tensor("dstate", s, (p.B, p.H, p.d, p.d), torch.float32, q.device)
-        keep = _with_workspace(p, int(lib().salad_gated_delta_workspace_bytes(C.byref(p), 1)), workspace, q.device)
-        _check(lib().salad_gated_delta_bwd(C.byref(p)))
-        del keep
-        return (*grads, s)
-    return _call_on(q.device, call)
+    def make():
+        shape = (v.shape[0], v.shape[1], v.shape[3], v.shape[3])
+        grads = tuple(torch.empty_like(like) if given is None else given
+                      for given, like in ((dq, q), (dk, k), (dv, v), (dg, g), (dbeta, beta)))
+        s = torch.empty(shape, dtype=torch.float32, device=q.device) if dstate is None else dstate
+        return _pack_delta, (*head, 0, s_in, 0, ln, _tensor("dout", dout, v.shape, q.dtype, index),
+                             _tensor("dstate_out", dstate_out, shape, torch.float32, index, True),
+                             *(_tensor(n, x, y.shape, y.dtype, index) for n, x, y in zip(("dq", "dk", "dv", "dg", "dbeta"), grads, (q, k, v, g, beta))),
+                             _tensor("dstate", s, shape, torch.float32, index)), (*grads, s)
+    L = lib()
+    return _run(index, make, L.salad_gated_delta_bwd, L.salad_gated_delta_workspace_bytes, 1, workspace)

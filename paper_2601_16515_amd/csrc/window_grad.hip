@@ -11,6 +11,7 @@
 // without leaving the registers.  Each own row's sum runs over the streamed rows in order: no atomics, the same bits every time.
 // P and dS are rounded to bf16 for the products (half a step, 2^-9, as the results are); sums and accumulators are fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "causal.h"
 
@@ -163,27 +164,27 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
         for (int e = 0; e < 16; ++e) { acc1[i][e] = 0.f; if (KEYS) acc2[i][e] = 0.f; }
     const float c2 = a.scale * LOG2E;
 
-    auto step = [&](const int i, const int buf) {
-        __syncthreads();
-        if (i + 1 < str.n) issue(i + 1, buf ^ 1);
-        int head, y0;
-        where(i, head, y0);
+    // The products of one streamed tile; full: every pair is visible.  Where keys own, with registers for it, that is a stretch of code of its
+    // own without branches, whose matrix products, exponentials and LDS reads can be put side by side.
+    auto products = [&](auto full, const int y0, const int buf) __attribute__((always_inline)) {
         const u16 *T1 = Yb[buf], *T2 = Yb[buf] + TILE;
-        // positions of the streamed rows y0..y0+63, and whether all, or none, of the wave's pairs are visible
-        const int ybase = KEYS ? sp.off : 0, ya = ybase + y0, yb = KEYS ? ybase + min(y0 + 63, ymax) : y0 + 63;
-        const int pa = KEYS ? ya : w0, pb = KEYS ? yb : w1, ja = KEYS ? w0 : ya, jb = KEYS ? w1 : yb;      // queries pa..pb, keys ja..jb
-        if (ja > pb || (ja >= a.sinks && jb <= pa - a.window)) return;
-        const bool full = jb <= pa && (ja > pb - a.window || jb < a.sinks) && (!KEYS || y0 + 63 <= ymax);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             f32x16 s, dp;
 #pragma unroll
             for (int e = 0; e < 16; ++e) { s[e] = 0.f; dp[e] = 0.f; }
+            bf16x8 y1[NS], y2[NS];
 #pragma unroll
             for (int st = 0; st < NS; ++st) {
                 const int off = (kt * 32 + kappa) * D + (((2 * st + hh) ^ sigma<D>(kappa)) << 3);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(T1 + off), x1[st].v, s, 0, 0, 0);
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(T2 + off), x2[st].v, dp, 0, 0, 0);
+                y1[st] = *reinterpret_cast<const bf16x8 *>(T1 + off);
+                y2[st] = *reinterpret_cast<const bf16x8 *>(T2 + off);
+            }
+            if (KEYS) __builtin_amdgcn_sched_barrier(0);        // all requested ahead of the first product (1392 -> 1330 us at 12 heads, N = 12480)
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y1[st], x1[st].v, s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y2[st], x2[st].v, dp, 0, 0, 0);
             }
             Frag pf[2], sf[2];
 #pragma unroll
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
                     float x = __builtin_amdgcn_exp2f(fmaf(s[e + f], c2, -ls));
                     float y = x * (dp[e + f] - dl);
                     if (!full) {
-                        const bool see = KEYS ? y0 + yr <= ymax && window_sees(a, pos, ybase + y0 + yr) : window_sees(a, y0 + yr, pos);
+                        const bool see = KEYS ? y0 + yr <= ymax && window_sees(a, pos, (KEYS ? sp.off : 0) + y0 + yr) : window_sees(a, y0 + yr, pos);
                         x = see ? x : 0.f;
                         y = see ? y : 0.f;
                     }
@@ -226,10 +227,28 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
                 }
         }
     };
+    auto step = [&](const int i, const int buf) {
+        __syncthreads();
+        if (i + 1 < str.n) issue(i + 1, buf ^ 1);
+        int head, y0;
+        where(i, head, y0);
+        // positions of the streamed rows y0..y0+63, and whether all, or none, of the wave's pairs are visible
+        const int ybase = KEYS ? sp.off : 0, ya = ybase + y0, yb = KEYS ? ybase + min(y0 + 63, ymax) : y0 + 63;
+        const int pa = KEYS ? ya : w0, pb = KEYS ? yb : w1, ja = KEYS ? w0 : ya, jb = KEYS ? w1 : yb;      // queries pa..pb, keys ja..jb
+        if (ja > pb || (ja >= a.sinks && jb <= pa - a.window)) return;
+        const bool full = jb <= pa && (ja > pb - a.window || jb < a.sinks) && (!KEYS || y0 + 63 <= ymax);
+        if constexpr (!KEYS) products(full, y0, buf);
+        else if (full) products(std::true_type(), y0, buf);
+        else products(std::false_type(), y0, buf);
+    };
     if (str.n > 0) issue(0, 0);
-    for (int i = 0; i < str.n; i += 2) {
-        step(i, 0);
-        if (i + 1 < str.n) step(i + 1, 1);
+    if constexpr (KEYS) {
+        for (int i = 0; i < str.n; ++i) step(i, i & 1);
+    } else {
+        for (int i = 0; i < str.n; i += 2) {
+            step(i, 0);
+            if (i + 1 < str.n) step(i + 1, 1);
+        }
     }
     if (KEYS && pieces > 1) {       // a piece's sums: joined afterwards, in order
         float *part = a.sink_part + ((((size_t)outer * window_sink_tiles_of(a) + tile) * pieces + piece) * 2 * 128 + wave * 32 + l32) * D;

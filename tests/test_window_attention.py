@@ -363,3 +363,14 @@ def test_the_binding_checks_tensors():
         sb.salad_window_attn_fwd(q, k, v, 0)
     with pytest.raises(TypeError):
         sb.salad_window_attn_fwd(q.half(), k.half(), v.half(), 4)
+
+
+def test_packed_parameters_have_the_structures_layout():
+    """The binding packs the parameter structures; their sizes, and the last field's place, are those of the C structures."""
+    for pack, cls, ints in ((sb._pack_window, sb.WindowParams, 10), (sb._pack_delta, sb.DeltaParams, 6)):
+        n = len(cls._fields_)
+        values = list(range(1, n + 1))
+        data = pack(*values)
+        assert len(data) == C.sizeof(cls)
+        p = cls.from_buffer_copy(data)
+        assert [getattr(p, f[0]) for f in cls._fields_] == values
