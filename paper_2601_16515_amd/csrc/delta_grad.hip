@@ -70,51 +70,61 @@ __global__ __launch_bounds__(256) void delta_x_kernel(DeltaArgs a)
 
 // ---- the rest, every chunk at once ----------------------------------------------------------------------------
 // Transposed: a lane's column is token i = 16 wave + l % 16, rows are key channels or the other token.  The contractions over the value
-// channels go in blocks of 32 through LDS.
+// channels go in blocks of 32 through LDS, the next block on its way meanwhile.  8 waves: 4 of the tokens by 2 of the key channels; of the products
+// over pairs of tokens one half takes A's, the other P's.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
+__global__ __launch_bounds__(512, 1) void delta_grad_kernel(DeltaArgs a)
 {
-    constexpr int P = planes_of<T>(), NK = D / 32, NA = D / 16, SP = D + 8, UP = 72, SPL = 32 * SP, UPL = 32 * UP;
+    constexpr int P = planes_of<T>(), NK = D / 32, NA = D / 32, SP = D + 8, UP = 72, SPL = 32 * SP, UPL = 32 * UP;
     using Tile = Tile64<T, D>;
     extern __shared__ __attribute__((aligned(16))) u16 lds[];
     u16 *S0 = lds, *S1 = S0 + 3 * SPL, *Ut = S1 + 3 * SPL, *Rt = Ut + 3 * UPL;          // [32][D], [32][D], [32][64], [32][64]
     u16 *X = lds, *Et = X + P * Tile::PLANE, *Pt = Et + P * 64 * UP;                    // afterwards: K or Q [64][D]; E and dP [token i][token j]
-    __shared__ float cols[4][64], red[4], fin[64];
+    __shared__ float cols[8][64], red[8], fin[2][64], fdb[2][64];
     const int ch = blockIdx.x % a.chunks, bh = blockIdx.x / a.chunks, b = bh / a.H, h = bh - b * a.H, G = a.H / a.Hk, hk = h / G;
     const int valid = min(delta_len(a, b) - ch * 64, 64);
     if (valid <= 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, l4 = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 & 3, half = wave8 >> 2, l16 = lane & 15, l4 = lane >> 4;
     const size_t at = (size_t)bh * a.chunks + ch, row0 = ((size_t)b * a.Hk + hk) * a.N + (size_t)ch * 64, vrow0 = (size_t)bh * a.N + (size_t)ch * 64;
     const T *qp = reinterpret_cast<const T *>(a.q) + row0 * D, *kp = reinterpret_cast<const T *>(a.k) + row0 * D;
     const T *gp = reinterpret_cast<const T *>(a.dout) + vrow0 * D, *vp = reinterpret_cast<const T *>(a.v) + vrow0 * D;
     T *dvp = reinterpret_cast<T *>(a.dv) + vrow0 * D;
     const int tok = 16 * wave + l16;
     const bool live = tok < valid;
-    f32x4 qs[NA], ks[NA], ke[NA], ru[4], ou[4];
+    const int a0 = half * (D / 2);                                      // this half's key channels
+    f32x4 qs[NA], ks[NA], ke[NA], pu[4];                                // pu: dR U^T, or dO U^T
 #pragma unroll
     for (int x = 0; x < NA; ++x) qs[x] = ks[x] = ke[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) ru[x] = ou[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < 4; ++x) pu[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     float sds = 0.f, rv = 0.f;                                          // S_0 . dS, dR . v
     const float beta = a.gate[at].beta[tok];
+    constexpr int NS = 8 * D / 512;
+    f32x4 xs[NS], ys[NS], xu, xr;
+    auto load = [&](int cb) __attribute__((always_inline)) {
+        const float *s0 = a.s0 + (at * D + cb * 32) * D, *s1 = a.ds1 + (at * D + cb * 32) * D;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) { xs[i] = load4(s0 + (i * 512 + tid) * 4); ys[i] = load4(s1 + (i * 512 + tid) * 4); }
+        xu = load4(a.u + (at * D + cb * 32) * 64 + tid * 4);
+        xr = load4(a.dr + (at * D + cb * 32) * 64 + tid * 4);
+    };
+    load(0);
     for (int cb = 0; cb < D / 32; ++cb) {
-        const float *s0 = reinterpret_cast<const float *>(a.s0) + (at * D + cb * 32) * D, *s1 = a.ds1 + (at * D + cb * 32) * D;
-        const float *up = reinterpret_cast<const float *>(a.u) + (at * D + cb * 32) * 64, *rp = a.dr + (at * D + cb * 32) * 64;
-        __syncthreads();
-        for (int i = tid; i < 8 * D; i += 256) {
-            const f32x4 x = load4(s0 + i * 4), y = load4(s1 + i * 4);
-            sds += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
-            put4<3>(S0 + (i * 4 / D) * SP + i * 4 % D, SPL, x);
-            put4<3>(S1 + (i * 4 / D) * SP + i * 4 % D, SPL, y);
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const int e = (i * 512 + tid) * 4;
+            sds += xs[i][0] * ys[i][0] + xs[i][1] * ys[i][1] + xs[i][2] * ys[i][2] + xs[i][3] * ys[i][3];
+            put4<3>(S0 + (e / D) * SP + e % D, SPL, xs[i]);
+            put4<3>(S1 + (e / D) * SP + e % D, SPL, ys[i]);
         }
-        for (int i = tid; i < 512; i += 256) {
-            put4<3>(Ut + (i / 16) * UP + i % 16 * 4, UPL, load4(up + i * 4));
-            put4<3>(Rt + (i / 16) * UP + i % 16 * 4, UPL, load4(rp + i * 4));
-        }
-        __syncthreads();
+        put4<3>(Ut + (tid / 16) * UP + tid % 16 * 4, UPL, xu);
+        put4<3>(Rt + (tid / 16) * UP + tid % 16 * 4, UPL, xr);
+        lds_barrier();
+        load(min(cb + 1, D / 32 - 1));
         const Op<P> go = frag_g(gp + (size_t)min(tok, valid - 1) * D + cb * 32 + 8 * l4, live);
         const Op<3> ui = frag_t<3>(Ut, UPL, UP, 16 * wave, 0, lane), ri = frag_t<3>(Rt, UPL, UP, 16 * wave, 0, lane);
-        {   // dv = beta dR: this lane's token and 8 value channels
+        if (half == 0) {        // dv = beta dR: this lane's token and 8 value channels
             const size_t at8 = (size_t)min(tok, valid - 1) * D + cb * 32 + 8 * l4;
             const f32x4 va = load4(vp + at8), vb = load4(vp + at8 + 4);
             f32x4 x, y;
@@ -131,61 +141,57 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
         }
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
-            const Op<3> f0 = frag_t<3>(S0, SPL, SP, 16 * x, 0, lane);
+            const Op<3> f0 = frag_t<3>(S0, SPL, SP, a0 + 16 * x, 0, lane);
             mma(qs[x], f0, go);
             mma(ks[x], f0, ri);
-            mma(ke[x], frag_t<3>(S1, SPL, SP, 16 * x, 0, lane), ui);
+            mma(ke[x], frag_t<3>(S1, SPL, SP, a0 + 16 * x, 0, lane), ui);
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x)
             if (x <= wave) {
                 const Op<3> uj = frag_t<3>(Ut, UPL, UP, 16 * x, 0, lane);
-                mma(ru[x], uj, ri);
-                mma(ou[x], uj, go);
+                if (half == 0) mma(pu[x], uj, ri);
+                else mma(pu[x], uj, go);
             }
     }
     const float gamma = a.gate[at].gamma[tok], tail = a.gate[at].tail[tok];
     const float2 bi = a.bsum[at * 64 + tok];
-    Op<P> ki[NK], qi[NK];
+    Op<P> ti[NK];                                                       // the token's key, or query
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-        ki[x] = frag_g(kp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, live);
-        qi[x] = frag_g(qp + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, live);
-    }
+    for (int x = 0; x < NK; ++x) ti[x] = frag_g((half == 0 ? kp : qp) + (size_t)min(tok, valid - 1) * D + x * 32 + 8 * l4, live);
     __syncthreads();                                                    // the blocks' tiles make room
     // pairs (i = own token, j): what A and P have to say
     float rows = 0.f, db = rv;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = kk, e = kk, dp = kk, cs = kk;
+        f32x4 kk = {0.f, 0.f, 0.f, 0.f}, e = kk, cs = kk;
         if (x <= wave) {
 #pragma unroll
-            for (int y = 0; y < NK; ++y) {
-                const Op<P> kj = frag_g(kp + (size_t)min(16 * x + l16, valid - 1) * D + y * 32 + 8 * l4, 16 * x + l16 < valid);
-                mma(kk, kj, ki[y]);
-                mma(qk, kj, qi[y]);
-            }
+            for (int y = 0; y < NK; ++y)
+                mma(kk, frag_g(kp + (size_t)min(16 * x + l16, valid - 1) * D + y * 32 + 8 * l4, 16 * x + l16 < valid), ti[y]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int j = 16 * x + 4 * l4 + r;
                 const float2 bj = a.bsum[at * 64 + j];
                 const float ratio = j <= tok ? expf((bi.x - bj.x) + (bi.y - bj.y)) : 0.f;
-                const float da = j < tok ? -ru[x][r] * ratio : 0.f;
-                e[r] = da * beta;
-                dp[r] = a.scale * ratio * ou[x][r];
-                cs[r] = j < tok ? e[r] * kk[r] + dp[r] * qk[r] : 0.f;   // by the decay between j and i; none from a token to itself
-                db += da * kk[r];
+                if (half == 0) {
+                    const float da = j < tok ? -pu[x][r] * ratio : 0.f;
+                    e[r] = da * beta;
+                    db += da * kk[r];
+                } else {
+                    e[r] = a.scale * ratio * pu[x][r];
+                }
+                cs[r] = j < tok ? e[r] * kk[r] : 0.f;                   // by the decay between j and i; none from a token to itself
                 rows += cs[r];
             }
         }
-        put4<P>(Et + tok * UP + 16 * x + 4 * l4, 64 * UP, e);
-        put4<P>(Pt + tok * UP + 16 * x + 4 * l4, 64 * UP, dp);
+        put4<P>((half == 0 ? Et : Pt) + tok * UP + 16 * x + 4 * l4, 64 * UP, e);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float c = cs[r];
 #pragma unroll
             for (int m = 1; m < 16; m <<= 1) c += __shfl_xor(c, m);
-            if (l16 == 0) cols[wave][16 * x + 4 * l4 + r] = c;
+            if (l16 == 0) cols[wave8][16 * x + 4 * l4 + r] = c;
         }
     }
     // products with the states: scales, and what reaches the decays
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
     for (int x = 0; x < NA; ++x) {
         f32x4 q4 = {0.f, 0.f, 0.f, 0.f}, k4 = q4;
-        if (live) { q4 = load4(qp + (size_t)tok * D + 16 * x + 4 * l4); k4 = load4(kp + (size_t)tok * D + 16 * x + 4 * l4); }
+        if (live) { q4 = load4(qp + (size_t)tok * D + a0 + 16 * x + 4 * l4); k4 = load4(kp + (size_t)tok * D + a0 + 16 * x + 4 * l4); }
         qs[x] *= a.scale * gamma;
         ks[x] *= -gamma;
         ke[x] *= tail;
@@ -213,18 +219,23 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) sds += __shfl_xor(sds, m);
     const float gend = a.gate[at].gamma[63];
-    if (lane == 0) red[wave] = end + gend * sds;
-    if (l4 == 0) {
-        fin[tok] = rows;
-        if (live) a.dbeta[vrow0 + tok] = db;
-    }
+    if (lane == 0) red[wave8] = end + gend * sds;
+    if (l4 == 0) { fin[half][tok] = rows; fdb[half][tok] = db; }
     Tile t;
-    t.load(kp, valid, tid);
-    t.store(X, tid);
+    if (tid < 256) {
+        t.load(kp, valid, tid);
+        t.store(X, tid);
+        t.load(qp, valid, tid);
+    }
     __syncthreads();
-    if (wave == 0) {                                                    // dg: the sums from each token to the end of the chunk
-        float d = fin[lane] - (cols[0][lane] + cols[1][lane] + cols[2][lane] + cols[3][lane]);
-        if (lane == 63) d += red[0] + red[1] + red[2] + red[3];
+    if (wave8 == 0) {                                                   // dbeta, and dg: the sums from each token to the end of the chunk
+        if (lane < valid) a.dbeta[vrow0 + lane] = fdb[0][lane] + fdb[1][lane];
+        float d = fin[0][lane] + fin[1][lane];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            d -= cols[w][lane];
+            if (lane == 63) d += red[w];
+        }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
             const float o = __shfl_down(d, m);
@@ -232,7 +243,6 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
         }
         if (lane < valid) a.dg[vrow0 + lane] = d;
     }
-    t.load(qp, valid, tid);
     Op<P> en[2], pn[2], et[2], pt[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -245,20 +255,20 @@ __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaArgs a)
     for (int x = 0; x < NA; ++x)
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            const Op<P> f = frag_t<P>(X, Tile::PLANE, Tile::PITCH, 16 * x, 32 * kt, lane);
+            const Op<P> f = frag_t<P>(X, Tile::PLANE, Tile::PITCH, a0 + 16 * x, 32 * kt, lane);
             mma(qs[x], f, pn[kt]);
             mma(ks[x], f, en[kt]);
             mma(ks[x], f, et[kt]);
         }
     __syncthreads();
-    t.store(X, tid);
+    if (tid < 256) t.store(X, tid);
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < NA; ++x) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) mma(ks[x], frag_t<P>(X, Tile::PLANE, Tile::PITCH, 16 * x, 32 * kt, lane), pt[kt]);
+        for (int kt = 0; kt < 2; ++kt) mma(ks[x], frag_t<P>(X, Tile::PLANE, Tile::PITCH, a0 + 16 * x, 32 * kt, lane), pt[kt]);
         if (live) {
-            const size_t c = 16 * x + 4 * l4;
+            const size_t c = a0 + 16 * x + 4 * l4;
             if (a.dq_part) {
                 store4(a.dq_part + (vrow0 + tok) * D + c, qs[x]);
                 store4(a.dk_part + (vrow0 + tok) * D + c, ks[x]);
@@ -304,7 +314,7 @@ hipError_t run(const DeltaArgs &a, hipStream_t st)
     const dim3 all(a.B * a.H * a.chunks);
     launch_kernel((delta_x_kernel<T, D>), all, dim3(256), x_bytes, st, a);
     if (const hipError_t e = launch_delta_chains(a, true, st)) return e;
-    launch_kernel((delta_grad_kernel<T, D>), all, dim3(256), grad_bytes, st, a);
+    launch_kernel((delta_grad_kernel<T, D>), all, dim3(512), grad_bytes, st, a);
     if (a.dq_part) {
         const long long total = (long long)a.B * a.Hk * a.N * D / 4;
         launch_kernel((delta_share_kernel<T>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, a, total);
