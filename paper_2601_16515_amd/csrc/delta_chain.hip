@@ -460,9 +460,21 @@ __global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int block
             const int row = wave * (D / 4) + 16 * x;
 #pragma unroll
             for (int r = 0; r < 4; ++r) c[x][r] = sum[(size_t)(row + 4 * l4 + r) * D + c0 + l16];
-            if (i > 1)
-                for (int k = 0; k < D; k += 4)
-                    c[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(BACK ? map[(size_t)(k + l4) * D + row + l16] : map[(size_t)(row + l16) * D + k + l4], S[k + l4][l16], c[x], 0, 0, 0);
+            if (i > 1) {
+                // step 4 kb + y of the contraction takes rows 16 kb + 4 l4 + y of S: a lane's operands are neighbours in M
+                f32x4 m[D / 16];
+#pragma unroll
+                for (int kb = 0; kb < D / 16; ++kb) {
+                    if (!BACK) m[kb] = load4(map + (size_t)(row + l16) * D + 16 * kb + 4 * l4);
+                    else
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) m[kb][y] = map[(size_t)(16 * kb + 4 * l4 + y) * D + row + l16];
+                }
+#pragma unroll
+                for (int kb = 0; kb < D / 16; ++kb)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) c[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[kb][y], S[16 * kb + 4 * l4 + y][l16], c[x], 0, 0, 0);
+            }
         }
         __syncthreads();
 #pragma unroll

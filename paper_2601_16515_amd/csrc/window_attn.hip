@@ -4,7 +4,7 @@
 //   lse = m + log sum_j exp(s_j - m)
 //
 // Three kernels:
-//   window_fwd_kernel    bf16, many queries: 128 queries of one head per workgroup, 64-key tiles through LDS
+//   window_fwd_kernel    bf16, many queries: 128 or 256 queries of one head per workgroup, 64-key tiles through LDS
 //   window_step_kernel   bf16, few queries against a long cache: the heads of a group and their tokens are the 32 rows of a
 //                        matrix product, the keys are dealt to waves and workgroups and joined afterwards
 //   window_f32_kernel    fp32
@@ -55,10 +55,10 @@ __device__ inline int kappa_of(int l) { return (l & 0x13) | ((l & 4) << 1) | ((l
 }  // namespace
 
 // ---- many queries -----------------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256, 2) void window_fwd_kernel(WindowArgs a, int ntiles, int total, int per_xcd)
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void window_fwd_kernel(WindowArgs a, int ntiles, int total, int per_xcd)
 {
-    constexpr int NS = D / 16, NDT = D / 32, CH = D / 8, TILE = 64 * D, RPP = 256 / CH, NP = 64 / RPP;
+    constexpr int NS = D / 16, NDT = D / 32, CH = D / 8, TILE = 64 * D, RPP = 64 * WAVES / CH, NP = 64 / RPP, ROWS = 32 * WAVES;
     __shared__ __attribute__((aligned(1024))) u16 Kb[2 * TILE];
     __shared__ __attribute__((aligned(1024))) u16 Vb[2 * TILE];
     // consecutive workgroups go to the 8 XCDs in turn: each gets a contiguous range, so that neighbouring tiles of a head share an L2
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_kernel(WindowArgs a, int nt
     const int bh = L / ntiles, tile = ntiles - 1 - (L - bh * ntiles);    // the last queries see most
     const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
     const WindowSpan sp = window_span(a, b);
-    const int n0 = tile * 128;
+    const int n0 = tile * ROWS;
     if (n0 >= sp.qlen) return;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hh = lane >> 5;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_kernel(WindowArgs a, int nt
     const int qrow = live ? n : sp.qlen - 1;
     const int p = sp.off + qrow;
     const int pw0 = sp.off + min(n0 + wave * 32, sp.qlen - 1), pw1 = sp.off + min(n0 + wave * 32 + 31, sp.qlen - 1);
-    const int p1 = sp.off + min(n0 + 127, sp.qlen - 1);
+    const int p1 = sp.off + min(n0 + ROWS - 1, sp.qlen - 1);
     const KeyTiles kt_list(a, sp.off + n0, p1, 64);
 
     Frag qf[NS];
@@ -95,9 +95,9 @@ __global__ __launch_bounds__(256, 2) void window_fwd_kernel(WindowArgs a, int nt
             const int r = i * RPP + lr;
             const size_t row = window_row(a, min(t * 64 + r, p1));       // no row that no query sees: it may never have been written
             __builtin_amdgcn_global_load_lds(GLB_PTR(kb + row * D + (pc ^ sigma_k<D>(r)) * 8),
-                                             LDS_PTR(Kb + buf * TILE + (i * 256 + wave * 64) * 8), 16, 0, 0);
+                                             LDS_PTR(Kb + buf * TILE + (i * 64 * WAVES + wave * 64) * 8), 16, 0, 0);
             __builtin_amdgcn_global_load_lds(GLB_PTR(vb + row * D + (pc ^ sigma_v<D>(r)) * 8),
-                                             LDS_PTR(Vb + buf * TILE + (i * 256 + wave * 64) * 8), 16, 0, 0);
+                                             LDS_PTR(Vb + buf * TILE + (i * 64 * WAVES + wave * 64) * 8), 16, 0, 0);
         }
     };
 
@@ -224,12 +224,20 @@ __global__ __launch_bounds__(256, 2) void window_fwd_kernel(WindowArgs a, int nt
     if (a.lse && hh == 0) a.lse[(size_t)bh * a.Nq + qrow] = l_tot == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_tot)) * LN2;
 }
 
+template <int D, int WAVES>
+static void launch_fwd(const WindowArgs &a, hipStream_t st)
+{
+    const int ntiles = (a.Nq + 32 * WAVES - 1) / (32 * WAVES), total = a.B * a.H * ntiles, per_xcd = (total + 7) / 8;
+    launch_kernel((window_fwd_kernel<D, WAVES>), dim3(per_xcd * 8), dim3(64 * WAVES), 0, st, a, ntiles, total, per_xcd);
+}
+
 hipError_t launch_window_fwd_bf16(const WindowArgs &a, hipStream_t st)
 {
-    const int ntiles = (a.Nq + 127) / 128;
-    const int total = a.B * a.H * ntiles, per_xcd = (total + 7) / 8;
-    if (a.D == 128) launch_kernel((window_fwd_kernel<128>), dim3(per_xcd * 8), dim3(256), 0, st, a, ntiles, total, per_xcd);
-    else launch_kernel((window_fwd_kernel<64>), dim3(per_xcd * 8), dim3(256), 0, st, a, ntiles, total, per_xcd);
+    // 8 waves share a tile of K and V where that leaves two workgroups for each compute unit: 12 heads, N = 32760, d = 128 1677 -> 1593 us.  At
+    // d = 64 a workgroup of 4 leaves room for a third beside it, and 8 are slower (164 -> 205 us at 24 heads, N = 4095).
+    if (a.D == 128 && (long long)a.B * a.H * ((a.Nq + 255) / 256) >= 512) launch_fwd<128, 8>(a, st);
+    else if (a.D == 128) launch_fwd<128, 4>(a, st);
+    else launch_fwd<64, 4>(a, st);
     return take_launch_status();
 }
 

@@ -112,6 +112,8 @@ SHAPES = [
     (1, 3, 3, 130, 128, None, True, "alike"),
     (3, 4, 2, 200, 64, [200, 64, 129], True, "plain"),
     (1, 2, 1, 321, 128, None, True, "plain"),
+    (1, 2, 1, 1100, 64, None, True, "plain"),                # groups of chunks side by side
+    (2, 1, 1, 1100, 128, [1100, 70], True, "edges"),         # ... and a sample whose later groups are empty
 ]
 IDS = lambda s: "-".join(map(str, s[:5])) + "-" + s[7]  # noqa: E731
 
