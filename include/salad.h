@@ -310,6 +310,8 @@ salad_status salad_window_cache_append(const void *k_new, const void *v_new, voi
  *   states     fp32 [B,H,d,d].  state_in NULL: zeros.  state_out NULL: not wanted; it may be state_in itself (in place).
  *   lens       device int32 [B] or NULL (= N): tokens of each sample of a padded batch.  What lies behind is not read and left as it was;
  *              a sample without tokens hands its state on.  Values outside 0..N are taken as the nearer end.
+ * A value that is not finite reaches the state and so every later token of its sample and head; beyond 32 tokens also earlier ones of its
+ * chunk of 64.
  * Up to 32 tokens go one after the other with the state in registers; more go in chunks of 64 on the matrix cores.  The
  * two agree up to rounding.  Everything in the chain of states is fp32, or split so that it keeps fp32's bits.  No atomics: the same bits for
  * the same call. */

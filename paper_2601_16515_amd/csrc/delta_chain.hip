@@ -6,7 +6,9 @@
 // accumulators is an operand of the next as it stands (delta_planes.h): the chain never leaves its wave's registers.  What all waves
 // read, K, T, V and the decays, lies in LDS, a chunk's while the next one's is on its way: 4 more waves, one on each SIMD, load it, and
 // forward compute O = scale gamma Q S + P U from the operands that the chain leaves behind.
-// 132 products deep (d = 128; backward 180), the chain is bound by the matrix cores' issue: 16 cycles each, one wave to a SIMD.
+// A chunk takes 2.55 us at d = 128, about 6100 cycles: 132 products of 16 cycles each (backward 180) and about 400 vector
+// instructions, most of them splits into planes, one behind the other in one wave, with 490 of the helper on the same SIMD and the latency of
+// LDS between them.  Neither memory (406 MB in 573 us at 12 heads, N = 32760) nor the chip's matrix rate is near its bound.
 //
 // Few heads leave most of the chip idle, so the chunks are cut into groups.  The state behind a group is linear in the one before it,
 // S' = M S + B: chains from zeros give B and chains from the unit matrix without values give M, for all groups at once; a short
@@ -27,7 +29,8 @@ template <typename T, int D, bool BACK> struct Shape {
     static constexpr int P = planes_of<T>();
     static constexpr int SL = P == 1 ? 4 : 2;                               // waves of the chain, 16 value channels each
     static constexpr int KBUFS = P == 1 ? 2 : 1;                            // K (and Q) of two chunks, where LDS has room
-    static constexpr int VP = 16 * SL + 8, UO = P == 1 ? 1 : 3; // pitch; planes of u as a factor of O
+    static constexpr int VP = 16 * SL + 8;                                  // pitch
+    static constexpr int UO = P == 1 ? 2 : 3;                               // planes of u as a factor of O: beside S and P in one, a third rounding would show
     static constexpr bool QTILE = BACK || P == 1;                           // Q goes through LDS
     static constexpr int THREADS = 64 * (SL + 4);
 };
@@ -85,14 +88,6 @@ __device__ inline f32x4 values(const float (*v)[VP], int row, int c, int lane)
     return x;
 }
 
-template <int P>
-__device__ inline Op<P> first_planes(const Op<3> &f)
-{
-    Op<P> o;
-#pragma unroll
-    for (int i = 0; i < P; ++i) o.p[i] = f.p[i];
-    return o;
-}
 __device__ inline Op<3> tri_op(const u16 *t, int piece, int lane)
 {
     Op<3> f;
@@ -435,7 +430,7 @@ __global__ __launch_bounds__((Shape<T, D, false>::THREADS), 1) void delta_sum_ke
 }
 
 // The states that the groups start from: S <- M S + B from group to group (backward: M transposed, from the last).  A workgroup has 16 value
-// channels; S is in LDS, the products are fp32.
+// channels; S is in LDS, the products are fp32.  6 groups of 12 heads, d = 128: 19 us (35 with operands that are no neighbours in memory).
 template <int D>
 __global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int blocks)
 {
@@ -490,7 +485,9 @@ __global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int block
 }
 
 // Groups: as many as shorten the passes.  One pass of all chunks without groups; with G groups one of a G-th for B and M, and one
-// of a G-th for the rest, each as often as its workgroups fill the chip's 256 compute units.
+// of a G-th for the rest, each as often as its workgroups fill the chip's 256 compute units; 4 chunks of time for a step of the start kernel.
+// 12 heads, 512 chunks, d = 128: 1303 us in one group, 244 + 19 + 250 in groups.  Fewer than 8 chunks a group, or less than a fifth
+// to win, leave one group: the sum and start kernels cost that much.
 int delta_groups(const DeltaArgs &a, bool backward)
 {
     const int parts = a.D / (a.bf16 ? 64 : 32);

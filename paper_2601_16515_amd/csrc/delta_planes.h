@@ -144,8 +144,6 @@ __device__ inline f32x4 load4(const u16 *p)
 __device__ inline f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
 __device__ inline float load1(const u16 *p) { return __uint_as_float((uint32_t)*p << 16); }
 __device__ inline float load1(const float *p) { return *p; }
-__device__ inline void store1(u16 *p, float x) { *p = (u16)pack2(x, 0.f); }
-__device__ inline void store1(float *p, float x) { *p = x; }
 __device__ inline void store4(u16 *p, f32x4 x) { *reinterpret_cast<u32x2 *>(p) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])}; }
 __device__ inline void store4(float *p, f32x4 x) { *reinterpret_cast<f32x4 *>(p) = x; }
 
