@@ -57,6 +57,13 @@ struct KeyTiles {
     __device__ int tile(int i) const { return i < ns ? i : w0 + (i - ns); }
 };
 
+// Barrier behind loads that go straight into LDS: each wave waits for its own first, which a barrier alone leaves to chance.
+__device__ inline void landed_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 constexpr int STEP_ROWS = 32;       // rows (heads of a group x tokens) of a step-kernel workgroup
 int window_step_splits(int B, int Hk, int row_tiles, int max_keys);     // 0: the call takes the tile kernel
 bool window_takes_step(const WindowArgs &a);

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_fwd_kernel(WindowArgs a,
     const float c2 = a.scale * LOG2E;
 
     auto step = [&](const int i, const int buf) {
-        __syncthreads();   // tile `buf` has landed (the fence waits for the LDS loads); buf^1 is free
+        landed_barrier();  // tile `buf` is there; buf^1 is free
         if (i + 1 < kt_list.n) issue(kt_list.tile(i + 1), buf ^ 1);
         const int j0 = kt_list.tile(i) * 64;
         if (j0 > pw1 || (j0 >= a.sinks && j0 + 63 <= pw0 - a.window)) return;          // nothing for this wave

@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
         }
     };
     auto step = [&](const int i, const int buf) {
-        __syncthreads();
+        landed_barrier();
         if (i + 1 < str.n) issue(i + 1, buf ^ 1);
         int head, y0;
         where(i, head, y0);
