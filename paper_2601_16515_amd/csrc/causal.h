@@ -102,7 +102,7 @@ struct DeltaArgs {
     struct DeltaGate *gate;
     float2 *bsum;                   // [64] each: running sum of g as two floats
     u16 *tf, *ttf;                  // T = (I + A)^-1 and (backward) its transpose, operands in three planes
-    u16 *pf;                        // forward: P, operand in one plane for bf16 tensors, three for fp32
+    u16 *pf;                        // forward: P, operand in two planes for bf16 tensors, three for fp32
     int groups, per_group;          // the chunks are cut into groups whose chains run side by side
     float *gsum, *gmap, *gstart;    // [BH][groups][D][D]: a group's chain from zeros, its linear map, and the state it starts from
     float *gsum_b, *gstart_b;       // backward: the same of the gradients' chain (its map is the transpose)

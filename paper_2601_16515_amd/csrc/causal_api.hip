@@ -153,7 +153,7 @@ size_t delta_ws(DeltaArgs &a, bool backward, char *ws)
         }
     }
     if (!backward) {
-        take(a.pf, n * (a.bf16 ? 1 : 3) * TRI * sizeof(u16));
+        take(a.pf, n * (a.bf16 ? 2 : 3) * TRI * sizeof(u16));
     } else {
         take(a.ttf, n * 3 * TRI * sizeof(u16));
         take(a.s0, n * D * D * sizeof(float));

@@ -30,7 +30,7 @@ template <typename T, int D, bool BACK> struct Shape {
     static constexpr int SL = P == 1 ? 4 : 2;                               // waves of the chain, 16 value channels each
     static constexpr int KBUFS = P == 1 ? 2 : 1;                            // K (and Q) of two chunks, where LDS has room
     static constexpr int VP = 16 * SL + 8;                                  // pitch
-    static constexpr int UO = P == 1 ? 2 : 3;                               // planes of u as a factor of O: beside S and P in one, a third rounding would show
+    static constexpr int UO = out_planes<T>();
     static constexpr bool QTILE = BACK || P == 1;                           // Q goes through LDS
     static constexpr int THREADS = 64 * (SL + 4);
 };
@@ -290,7 +290,8 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
         if (BACK) qr.store_swizzled(lds.q[i & (H::KBUFS - 1)], t);
     };
     // O: what it takes besides the chain's operands, loaded in its chunk, used in the next
-    Op<P> pf[2], qn[P == 1 ? 1 : NK];
+    Op<H::UO> pf[2];
+    Op<P> qn[P == 1 ? 1 : NK];
     float gamma = 0.f;
     auto load_out = [&](int i) __attribute__((always_inline)) {
         const int ch = chunk_of(i), valid = valid_of(ch);
@@ -298,8 +299,8 @@ __device__ inline void helper(const DeltaArgs &a, const Job &j, ChainLds<T, D, B
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-                pf[kt].p[p] = *reinterpret_cast<const bf16x8 *>(a.pf + at * (P * TRI) + p * TRI + (tri_lower(w, w < 2 ? 0 : kt) * 64 + lane) * 8);
+            for (int p = 0; p < H::UO; ++p)
+                pf[kt].p[p] = *reinterpret_cast<const bf16x8 *>(a.pf + at * (H::UO * TRI) + p * TRI + (tri_lower(w, w < 2 ? 0 : kt) * 64 + lane) * 8);
         gamma = a.scale * a.gate[at].gamma[16 * w + l16];
         if constexpr (H::QTILE) qr.load_clamped(q + (size_t)ch * 64 * D, valid - 1, t);
         else

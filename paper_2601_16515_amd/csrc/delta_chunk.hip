@@ -5,7 +5,7 @@
 //   S_64 = gamma_63 S_0 + K^T (tail u),  tail_i = e^(b_63 - b_i),     O = scale gamma Q S_0 + P U,  P_ij = scale e^(b_i - b_j) q_i.k_j  (j <= i).
 // T = (I + A)^-1 and P do not depend on the state: delta_chunk_kernel here computes them for every chunk at once.  The states go from
 // chunk to chunk in delta_chain.hip.  All exponents are differences of sums held in 64 bits; T keeps fp32 (three planes), P for bf16
-// tensors is rounded to bf16 (half a step of each term of O).
+// tensors two.
 // 12 heads, N = 32760, d = 128, bf16: 120 us for 406 MB of inputs and outputs, of which this kernel moves about half: the inverse's 16-token
 // blocks wait for each other and for LDS, two workgroups to a compute unit.
 #include <algorithm>
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256, 2) void delta_chunk_kernel(DeltaArgs a)
             out(three, a.ttf + at * (3 * TRI), tri_upper(wave, kt), f32x4{X[j][tok], X[j + 1][tok], X[j + 2][tok], X[j + 3][tok]},
                 f32x4{X[j + 16][tok], X[j + 17][tok], X[j + 18][tok], X[j + 19][tok]});
         if (!BWD && (kt == 0 || wave >= 2))
-            out(std::integral_constant<int, P>(), a.pf + at * (P * TRI), tri_lower(wave, kt), pp[2 * kt], pp[2 * kt + 1]);
+            out(std::integral_constant<int, out_planes<T>()>(), a.pf + at * (out_planes<T>() * TRI), tri_lower(wave, kt), pp[2 * kt], pp[2 * kt + 1]);
     }
 }
 
