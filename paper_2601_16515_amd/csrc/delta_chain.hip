@@ -8,7 +8,7 @@
 // forward compute O = scale gamma Q S + P U from the operands that the chain leaves behind.
 // A chunk takes 2.55 us at d = 128, about 6100 cycles: 132 products of 16 cycles each (backward 180) and about 400 vector
 // instructions, most of them splits into planes, one behind the other in one wave, with 490 of the helper on the same SIMD and the latency of
-// LDS between them.  Neither memory (406 MB in 573 us at 12 heads, N = 32760) nor the chip's matrix rate is near its bound.
+// LDS between them.  Neither memory (406 MB in 590 us at 12 heads, N = 32760) nor the chip's matrix rate is near its bound.
 //
 // Few heads leave most of the chip idle, so the chunks are cut into groups.  The state behind a group is linear in the one before it,
 // S' = M S + B: chains from zeros give B and chains from the unit matrix without values give M, for all groups at once; a short
