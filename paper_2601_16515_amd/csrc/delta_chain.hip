@@ -6,7 +6,7 @@
 // accumulators is an operand of the next as it stands (delta_planes.h): the chain never leaves its wave's registers.  What all waves
 // read, K, T, V and the decays, lies in LDS, a chunk's while the next one's is on its way: 4 more waves, one on each SIMD, load it, and
 // forward compute O = scale gamma Q S + P U from the operands that the chain leaves behind.
-// A chunk takes 2.55 us at d = 128, about 6100 cycles: 132 products of 16 cycles each (backward 180) and about 400 vector
+// A chunk takes 2.8 us at d = 128 (bf16 tensors; with O 3.1), about 6700 cycles: 132 products of 16 cycles each (backward 180) and about 400 vector
 // instructions, most of them splits into planes, one behind the other in one wave, with 490 of the helper on the same SIMD and the latency of
 // LDS between them.  Neither memory (406 MB in 590 us at 12 heads, N = 32760) nor the chip's matrix rate is near its bound.
 //
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int block
 
 // Groups: as many as shorten the passes.  One pass of all chunks without groups; with G groups one of a G-th for B and M, and one
 // of a G-th for the rest, each as often as its workgroups fill the chip's 256 compute units; 4 chunks of time for a step of the start kernel.
-// 12 heads, 512 chunks, d = 128: 1303 us in one group, 244 + 19 + 250 in groups.  Fewer than 8 chunks a group, or less than a fifth
+// 12 heads, 512 chunks, d = 128: 1303 us in one group, 244 + 20 + 269 in groups.  Fewer than 8 chunks a group, or less than a fifth
 // to win, leave one group: the sum and start kernels cost that much.
 int delta_groups(const DeltaArgs &a, bool backward)
 {

@@ -6,7 +6,7 @@
 // T = (I + A)^-1 and P do not depend on the state: delta_chunk_kernel here computes them for every chunk at once.  The states go from
 // chunk to chunk in delta_chain.hip.  All exponents are differences of sums held in 64 bits; T keeps fp32 (three planes), P for bf16
 // tensors two.
-// 12 heads, N = 32760, d = 128, bf16: 120 us for 406 MB of inputs and outputs, of which this kernel moves about half: the inverse's 16-token
+// 12 heads, N = 32760, d = 128, bf16: 126 us for 406 MB of inputs and outputs, of which this kernel moves about half: the inverse's 16-token
 // blocks wait for each other and for LDS, two workgroups to a compute unit.
 #include <algorithm>
 #include <type_traits>

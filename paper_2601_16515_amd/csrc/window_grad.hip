@@ -10,7 +10,7 @@
 //   acc1^T += Y1^T dS,  acc2^T += Y2^T P      (dq;   dk and dv)
 // without leaving the registers.  Each own row's sum runs over the streamed rows in order: no atomics, the same bits every time.
 // P and dS are rounded to bf16 for the products (half a step, 2^-9, as the results are); sums and accumulators are fp32.
-// 12 heads, N = 12480, d = 128: keys 1330 us, queries 700 us.  The keys' workgroup reads each streamed tile from LDS as often as the matrix
+// 12 heads, N = 12480, d = 128: keys 1361 us, queries 720 us (fastest 1255, 683).  The keys' workgroup reads each streamed tile from LDS as often as the matrix
 // cores need its products, so both take the same time, and its accumulators leave one wave to a SIMD to overlap them.
 #include <algorithm>
 #include <type_traits>
