@@ -31,29 +31,29 @@ def _delta(name, kind, B, H, Hk, d, N, dtype="bf16", ragged=False, state=False):
 def listed():
     return [
         # one viewer's stream, a token at a time from a rolling cache: the smallest call, latency counts
-        _window("window step: one stream", "window_step", 1, 12, 12, 128, 1, 1024, 4, context=3001),
+        _window("window step, one stream", "window_step", 1, 12, 12, 128, 1, 1024, 4, context=3001),
         # a server's batch of streams of very different ages, grouped heads, long window: the cache is read once
-        _window("window step: batch", "window_step", 64, 40, 8, 128, 1, 4096, 4, ragged=True, context=20000),
+        _window("window step, batch", "window_step", 64, 40, 8, 128, 1, 4096, 4, ragged=True, context=20000),
         # prompts of different lengths in one padded batch, grouped narrow heads
-        _window("window prompt: ragged batch", "window_prompt", 4, 24, 8, 64, 4095, 1000, 4, ragged=True),
+        _window("window prompt, ragged batch", "window_prompt", 4, 24, 8, 64, 4095, 1000, 4, ragged=True),
         # the 480p clip causally: four frames back, and the first frame stays visible
-        _window("window prompt: 480p clip", "window_prompt", 1, 12, 12, 128, 32760, 6240, 1560),
+        _window("window prompt, 480p clip", "window_prompt", 1, 12, 12, 128, 32760, 6240, 1560),
         # gradients of a reference run in fp32, odd length, grouped heads
-        _window("window gradients: f32", "window_train", 2, 4, 2, 64, 1025, 300, 16, dtype="f32"),
+        _window("window gradients, f32", "window_train", 2, 4, 2, 64, 1025, 300, 16, dtype="f32"),
         # a training step's gradients on a short clip (8 latent frames), three frames back and the first one
-        _window("window gradients: clip", "window_train", 1, 12, 12, 128, 12480, 4680, 1560),
+        _window("window gradients, clip", "window_train", 1, 12, 12, 128, 12480, 4680, 1560),
         # the state of one stream advances by a token
-        _delta("delta step: one stream", "delta_step", 1, 12, 12, 128, 1, state=True),
+        _delta("delta step, one stream", "delta_step", 1, 12, 12, 128, 1, state=True),
         # a server's batch: every state is read and written once
-        _delta("delta step: batch", "delta_step", 128, 40, 8, 128, 1, state=True),
+        _delta("delta step, batch", "delta_step", 128, 40, 8, 128, 1, state=True),
         # prompts of different lengths that continue from states, shared query and key heads, narrow heads
-        _delta("delta prompt: ragged batch", "delta_prompt", 4, 16, 8, 64, 4095, ragged=True, state=True),
+        _delta("delta prompt, ragged batch", "delta_prompt", 4, 16, 8, 64, 4095, ragged=True, state=True),
         # the 480p clip: few heads and a very long sequence
-        _delta("delta prompt: 480p clip", "delta_prompt", 1, 12, 12, 128, 32760),
+        _delta("delta prompt, 480p clip", "delta_prompt", 1, 12, 12, 128, 32760),
         # gradients of a reference run in fp32, odd length, shared query and key heads, state in and out
-        _delta("delta gradients: f32", "delta_train", 2, 4, 2, 64, 1025, dtype="f32", state=True),
+        _delta("delta gradients, f32", "delta_train", 2, 4, 2, 64, 1025, dtype="f32", state=True),
         # a training step's gradients on a short clip
-        _delta("delta gradients: clip", "delta_train", 1, 12, 12, 128, 12480),
+        _delta("delta gradients, clip", "delta_train", 1, 12, 12, 128, 12480),
     ]
 
 
