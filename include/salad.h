@@ -254,9 +254,10 @@ salad_status salad_gate_fwd_static(const void *x_t, const float *w_gate, float b
  *   out = softmax(scale q k^T) v over the keys it sees,   lse = log sum exp(scale q k^T)  (natural logarithm, fp32)
  * A query that sees no key (p < 0) gets zeros and lse = -infinity.
  *   q, out [B,H,Nq,d];  k, v [B,Hk,Nk,d], H a multiple of Hk: query head h reads key head h / (H / Hk).  d is 64 or 128.
- *   q_lens, kv_lens   device int32 [B] or NULL (= Nq, Nk): the samples of a padded batch.  Query rows behind q_len and key rows
- *                     behind kv_len are not read (they may hold anything, NaN included); rows of out, lse, dq behind q_len and
- *                     of dk, dv behind kv_len are left as they were.  Values outside 0..Nq and 0..Nk are taken as the nearer end.
+ *   q_lens, kv_lens   device int32 [B] or NULL (= Nq, Nk): the samples of a padded batch.  Query rows behind q_len, key rows
+ *                     behind kv_len, key rows that no query sees and (backward) queries that see no key may hold anything, NaN included;
+ *                     rows of out, lse, dq behind q_len and of dk, dv behind kv_len are left as they were, and dk and dv of a key that
+ *                     no query sees are zeros.  Values outside 0..Nq and 0..Nk are taken as the nearer end.
  *   ring              0: position j is row j of k and v.  1: k and v are a rolling cache: row j for j < sinks, else
  *                     sinks + (j - sinks) % (Nk - sinks).  kv_lens is then needed, counts all positions ever (up to 2^30), and
  *                     Nk >= sinks + window + Nq - 1 is needed for every key that some query sees to be there still.

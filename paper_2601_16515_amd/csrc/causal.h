@@ -40,6 +40,10 @@ __device__ inline int window_row(const WindowArgs &a, int j)
 {
     return !a.ring || j < a.sinks ? j : a.sinks + (int)((unsigned)(j - a.sinks) % (unsigned)(a.Nk - a.sinks));
 }
+// Keys that queries at positions p0..p1 see: the sinks and first..p1, with first = p0 - window + 1.  Tiles hold others, too; what is loaded for
+// those is the nearest that is seen, since P = 0 times an infinity or NaN (a row that was never written) would not be 0.
+__device__ inline int window_first(const WindowArgs &a, int p0) { return p0 - a.window + 1; }
+__device__ inline int window_nearest(const WindowArgs &a, int j, int first, int p1) { return min(j < a.sinks ? j : max(j, first), p1); }
 // Tiles of `size` keys (aligned at 0) that queries at positions p0..p1 see: those of the sinks, then those of the windows.
 struct KeyTiles {
     int ns, w0, n;

@@ -82,6 +82,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_fwd_kernel(WindowArgs a,
     const int p = sp.off + qrow;
     const int pw0 = sp.off + min(n0 + wave * 32, sp.qlen - 1), pw1 = sp.off + min(n0 + wave * 32 + 31, sp.qlen - 1);
     const int p1 = sp.off + min(n0 + ROWS - 1, sp.qlen - 1);
+    const int first = window_first(a, sp.off + n0);
     const KeyTiles kt_list(a, sp.off + n0, p1, 64);
 
     Frag qf[NS];
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_fwd_kernel(WindowArgs a,
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int r = i * RPP + lr;
-            const size_t row = window_row(a, min(t * 64 + r, p1));       // no row that no query sees: it may never have been written
+            const size_t row = window_row(a, window_nearest(a, t * 64 + r, first, p1));
             __builtin_amdgcn_global_load_lds(GLB_PTR(kb + row * D + (pc ^ sigma_k<D>(r)) * 8),
                                              LDS_PTR(Kb + buf * TILE + (i * 64 * WAVES + wave * 64) * 8), 16, 0, 0);
             __builtin_amdgcn_global_load_lds(GLB_PTR(vb + row * D + (pc ^ sigma_v<D>(r)) * 8),
@@ -263,6 +264,7 @@ __global__ __launch_bounds__(256, 2) void window_step_kernel(WindowArgs a, int r
     const size_t orow = ((size_t)b * a.H + h) * a.Nq + n;
     const int p = sp.off + n;
 
+    const int first = window_first(a, sp.off);
     const KeyTiles tiles(a, sp.off, sp.qlen > 0 ? sp.kv - 1 : -1, 32);
     const int t0 = (int)((long long)tiles.n * split / a.splits), t1 = (int)((long long)tiles.n * (split + 1) / a.splits);
 
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void window_step_kernel(WindowArgs a, int r
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const size_t r = window_row(a, min(t * 32 + i * RPP + lr, sp.kv - 1));
+            const size_t r = window_row(a, window_nearest(a, t * 32 + i * RPP + lr, first, sp.kv - 1));
             kr[i] = *reinterpret_cast<const u32x4 *>(kb + r * D + pc * 8);
             vv[i] = *reinterpret_cast<const u32x4 *>(vb + r * D + pc * 8);
         }
@@ -485,6 +487,7 @@ __global__ __launch_bounds__(256, 2) void window_f32_kernel(WindowArgs a, int ro
     const bool one = first / a.Nq == last / a.Nq;
     const int nlo = one ? first % a.Nq : 0, nhi = min(one ? last % a.Nq : a.Nq - 1, sp.qlen - 1);
     const int p1 = nhi >= nlo ? sp.off + nhi : -1;
+    const int seen = window_first(a, sp.off + nlo);
     const KeyTiles tiles(a, sp.off + nlo, p1, 16);
     const float *kb = reinterpret_cast<const float *>(a.k) + (size_t)bk * a.Nk * D + (lane % LPR) * 4;
     const float *vb = reinterpret_cast<const float *>(a.v) + (size_t)bk * a.Nk * D + (lane % LPR) * 4;
@@ -502,7 +505,7 @@ __global__ __launch_bounds__(256, 2) void window_f32_kernel(WindowArgs a, int ro
         f32x4 kv[NK], vv[NK];
 #pragma unroll
         for (int u = 0; u < NK; ++u) {
-            const size_t r = window_row(a, min(j0 + u * RPI + lane / LPR, p1));
+            const size_t r = window_row(a, window_nearest(a, j0 + u * RPI + lane / LPR, seen, p1));
             kv[u] = *reinterpret_cast<const f32x4 *>(kb + r * D);
             vv[u] = *reinterpret_cast<const f32x4 *>(vb + r * D);
         }

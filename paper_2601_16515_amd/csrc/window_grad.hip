@@ -50,15 +50,18 @@ template <int D> __device__ inline int sigma(int r) { return D == 128 ? ((r & 3)
 __device__ inline int kappa_of(int l) { return (l & 0x13) | ((l & 4) << 1) | ((l & 8) >> 1); }
 
 // The streamed rows of an own tile, in tiles of `size`: keys for queries at p0..p1, or the queries of all heads of the group for
-// keys j0..j1, of which this workgroup takes piece `piece` of `pieces`.
+// keys j0..j1, of which this workgroup takes piece `piece` of `pieces`.  Of a tile's rows only those are loaded that some own row sees, or is
+// seen by (rows lo..hi, and the sinks): what is not finite in others would outlast their P = 0.
 struct Stream {
     KeyTiles keys;
-    int first, per_head, t0, n;
-    __device__ Stream(const WindowArgs &a, const WindowSpan &sp, int p0, int p1, int size) : keys(a, p0, p1, size), first(0), per_head(0), t0(0), n(keys.n) {}
+    int lo, hi, first, per_head, t0, n;
+    __device__ Stream(const WindowArgs &a, const WindowSpan &sp, int p0, int p1, int size)
+        : keys(a, p0, p1, size), lo(window_first(a, p0)), hi(p1), first(0), per_head(0), t0(0), n(keys.n) {}
     __device__ Stream(const WindowArgs &a, const WindowSpan &sp, int j0, int j1, int size, int piece, int pieces) : keys(a, 0, -1, size)
     {
         const long long last_p = j0 < a.sinks ? (long long)sp.kv - 1 : min((long long)sp.kv - 1, (long long)j1 + a.window - 1);
-        const int lo = max(0, j0 - sp.off), hi = (int)min((long long)sp.qlen - 1, last_p - sp.off);
+        lo = max(0, j0 - sp.off);
+        hi = (int)min((long long)sp.qlen - 1, last_p - sp.off);
         first = lo / size;
         per_head = hi >= lo ? hi / size - first + 1 : 0;
         const long long all = (long long)per_head * (a.H / a.Hk);
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
         if (KEYS) { const int t = str.t0 + i; head = t / str.per_head; y0 = (str.first + t - head * str.per_head) * 64; }
         else { head = 0; y0 = str.keys.tile(i) * 64; }
     };
-    const int ymax = KEYS ? sp.qlen - 1 : t1;                           // no row behind the last that the call uses
+    auto nearest = [&](int y) { return KEYS ? min(max(y, str.lo), str.hi) : window_nearest(a, y, str.lo, str.hi); };
     auto issue = [&](int i, int buf) {
         int head, y0;
         where(i, head, y0);
@@ -150,12 +153,12 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
             const int rr = u * RPP + lr;
-            const size_t off = (hoff + min(y0 + rr, ymax)) * D + (pc ^ sigma<D>(rr)) * 8;
+            const size_t off = (hoff + nearest(y0 + rr)) * D + (pc ^ sigma<D>(rr)) * 8;
             __builtin_amdgcn_global_load_lds(GLB_PTR(Y1 + off), LDS_PTR(Yb[buf] + (u * 256 + wave * 64) * 8), 16, 0, 0);
             __builtin_amdgcn_global_load_lds(GLB_PTR(Y2 + off), LDS_PTR(Yb[buf] + TILE + (u * 256 + wave * 64) * 8), 16, 0, 0);
         }
         if (KEYS && wave < 2)
-            __builtin_amdgcn_global_load_lds(GLB_PTR((wave ? delta : lse) + hoff + min(y0 + lane, ymax)), LDS_PTR(&rowv[buf][wave][0]), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds(GLB_PTR((wave ? delta : lse) + hoff + nearest(y0 + lane)), LDS_PTR(&rowv[buf][wave][0]), 4, 0, 0);
     };
 
     const int kappa = kappa_of(l32), vr = 8 * hh + ((l32 >> 2) & 3);
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
                     float x = __builtin_amdgcn_exp2f(fmaf(s[e + f], c2, -ls));
                     float y = x * (dp[e + f] - dl);
                     if (!full) {
-                        const bool see = KEYS ? y0 + yr <= ymax && window_sees(a, pos, (KEYS ? sp.off : 0) + y0 + yr) : window_sees(a, y0 + yr, pos);
+                        const bool see = KEYS ? y0 + yr <= str.hi && window_sees(a, pos, (KEYS ? sp.off : 0) + y0 + yr) : window_sees(a, y0 + yr, pos);
                         x = see ? x : 0.f;
                         y = see ? y : 0.f;
                     }
@@ -235,10 +238,10 @@ __global__ __launch_bounds__(256, KEYS ? 1 : 2) void window_grad_kernel(WindowAr
         int head, y0;
         where(i, head, y0);
         // positions of the streamed rows y0..y0+63, and whether all, or none, of the wave's pairs are visible
-        const int ybase = KEYS ? sp.off : 0, ya = ybase + y0, yb = KEYS ? ybase + min(y0 + 63, ymax) : y0 + 63;
+        const int ybase = KEYS ? sp.off : 0, ya = ybase + y0, yb = KEYS ? ybase + min(y0 + 63, str.hi) : y0 + 63;
         const int pa = KEYS ? ya : w0, pb = KEYS ? yb : w1, ja = KEYS ? w0 : ya, jb = KEYS ? w1 : yb;      // queries pa..pb, keys ja..jb
         if (ja > pb || (ja >= a.sinks && jb <= pa - a.window)) return;
-        const bool full = jb <= pa && (ja > pb - a.window || jb < a.sinks) && (!KEYS || y0 + 63 <= ymax);
+        const bool full = jb <= pa && (ja > pb - a.window || jb < a.sinks) && (!KEYS || y0 + 63 <= str.hi);
         if constexpr (!KEYS) products(full, y0, buf);
         else if (full) products(std::true_type(), y0, buf);
         else products(std::false_type(), y0, buf);
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(256, 2) void window_grad_f32_kernel(WindowArgs a, i
     const bool live = r < own_rows;
     const int row = live ? r : own_rows - 1, base = KEYS ? 0 : sp.off, pos = base + row, t1 = base + min(r0 + 15, own_rows - 1);
     const Stream str = KEYS ? Stream(a, sp, r0, t1, 16, 0, 1) : Stream(a, sp, base + r0, t1, 16);
-    const int ymax = KEYS ? sp.qlen - 1 : t1;
+    auto nearest = [&](int y) { return KEYS ? min(max(y, str.lo), str.hi) : window_nearest(a, y, str.lo, str.hi); };
     f32x4 x1[NX], x2[NX], acc1[NX], acc2[NX];
 #pragma unroll
     for (int x = 0; x < NX; ++x) {
@@ -345,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void window_grad_f32_kernel(WindowArgs a, i
         f32x4 v1[NK], v2[NK];
 #pragma unroll
         for (int u = 0; u < NK; ++u) {
-            const size_t off = (hoff + min(y0 + u * RPI + lane / LPR, ymax)) * D + (lane % LPR) * 4;
+            const size_t off = (hoff + nearest(y0 + u * RPI + lane / LPR)) * D + (lane % LPR) * 4;
             v1[u] = *reinterpret_cast<const f32x4 *>(Y1 + off);
             v2[u] = *reinterpret_cast<const f32x4 *>(Y2 + off);
         }
@@ -371,9 +374,9 @@ __global__ __launch_bounds__(256, 2) void window_grad_f32_kernel(WindowArgs a, i
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int yr = y0 + 4 * g + e, yc = min(yr, ymax);
+            const int yr = y0 + 4 * g + e, yc = nearest(yr);
             const float ls = KEYS ? lse[hoff + yc] * LOG2E : own_lse, dl = KEYS ? delta[hoff + yc] : own_delta;
-            const bool see = KEYS ? yr <= ymax && window_sees(a, pos, sp.off + yr) : window_sees(a, yr, pos);
+            const bool see = KEYS ? yr <= str.hi && window_sees(a, pos, sp.off + yr) : window_sees(a, yr, pos);
             const float x = exp2f(fmaf(s[e], c2, -ls));
             s[e] = see ? x : 0.f;
             dp[e] = see ? x * (dp[e] - dl) : 0.f;

@@ -1,0 +1,99 @@
+"""The causal operators where their calls end: rows that nobody sees, rows behind a sample's last, calls that fill the chip."""
+import math
+
+import pytest
+import torch
+
+from paper_2601_16515_amd import binding as sb
+
+from . import causal_ref as ref
+from .gpu_util import say
+from .test_window_attention import _bound_out, _check_gradients, _inputs, _lens
+
+BOTH = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+
+
+def _hide(k, v, Nq, window, sinks, q_lens, kv_lens, ring=False):
+    """NaN and infinities in every row of k and v that no query of the sample sees, whether behind the last key, between the sinks and the
+    windows, or never written in a rolling cache; returns the rows [B, Nk] that are seen."""
+    B, Nk = k.shape[0], k.shape[2]
+    seen = torch.zeros(B, Nk, dtype=torch.bool, device=k.device)
+    for b in range(B):
+        ql, kv = (Nq if q_lens is None else q_lens[b]), (Nk if kv_lens is None else kv_lens[b])
+        some = ref.visible(ql, kv, Nq, Nk, window, sinks, k.device).any(0)
+        seen[b, ref.rows_of(kv, Nk, sinks, ring, k.device)[some]] = True
+        k[b, :, ~seen[b]], v[b, :, ~seen[b]] = math.inf, math.nan
+    return seen
+
+
+# B, H, Hk, Nq, Nk, d, window, sinks, q_lens, kv_lens: caches much longer than what the call's queries see
+GAPS = [
+    (1, 2, 1, 1, 97, 128, 40, 4, None, None),
+    (2, 4, 2, 3, 300, 64, 64, 5, [3, 1], [300, 120]),
+    (1, 2, 2, 1, 5000, 128, 3000, 130, None, None),                # keys in shares
+    (1, 2, 1, 40, 500, 128, 30, 4, None, None),
+    (2, 3, 1, 130, 700, 64, 77, 70, [130, 20], [700, 333]),
+    (4, 128, 2, 20, 300, 128, 50, 3, None, None),                  # enough queries for the widest tiles
+]
+
+
+@pytest.mark.gpu
+@BOTH
+@pytest.mark.parametrize("shape", GAPS, ids=lambda s: "-".join(map(str, s[:8])))
+def test_rows_that_no_query_sees_may_hold_anything(shape, dtype):
+    B, H, Hk, Nq, Nk, d, window, sinks, q_lens, kv_lens = shape
+    say(f"unseen rows {shape} {dtype}")
+    q, k, v, dout = _inputs(B, H, Hk, Nq, Nk, d, dtype, 20)
+    ql, kl = _lens(q_lens), _lens(kv_lens)
+    want, lse_want, cost = ref.window_attention(q, k, v, window, sinks, q_lens, kv_lens)
+    out, lse = torch.zeros_like(q), torch.zeros(B, H, Nq, device="cuda")
+    clean = sb.salad_window_attn_fwd(q, k, v, window, sinks, q_lens=ql, kv_lens=kl, out=out.clone(), lse=lse)
+    grads = [torch.zeros_like(t) for t in (q, k, v)]
+    g_want, g_cost, g_slack = ref.window_gradients(q, k, v, clean, lse, dout, window, sinks, q_lens, kv_lens)
+    seen = _hide(k, v, Nq, window, sinks, q_lens, kv_lens)
+    sb.salad_window_attn_fwd(q, k, v, window, sinks, q_lens=ql, kv_lens=kl, out=out, lse=lse)
+    assert torch.equal(out, clean)                                  # and clean holds the definition:
+    live = torch.arange(Nq, device="cuda") < (torch.full((B, 1), Nq, device="cuda") if ql is None else ql[:, None])
+    err = torch.where(live[:, None, :, None], (out.double() - want).abs(), 0.0)
+    assert (err <= _bound_out(want, cost, dtype, d, Nk)).all(), float(err.max())
+    err = (lse.double() - lse_want)[live[:, None].expand_as(lse)].abs()
+    assert (err < 2.0 ** -24 * (2 * d + Nk + 32) * 4).all()
+    sb.salad_window_attn_bwd(q, k, v, out, lse, dout, window, sinks, q_lens=ql, kv_lens=kl, dq=grads[0], dk=grads[1], dv=grads[2])
+    _check_gradients(grads, g_want, g_cost, g_slack, dtype, max(Nk, Nq * H // Hk))
+    for g in grads[1:]:                                             # rows that nobody sees have no gradient, whatever they hold
+        assert not g.transpose(1, 2)[~seen].any()
+
+
+@pytest.mark.gpu
+@BOTH
+@pytest.mark.parametrize("Nq,window,sinks,spare,kv", [(1, 40, 4, 60, 900), (5, 100, 3, 37, 700), (40, 64, 70, 200, 1000), (1, 2000, 0, 500, 9000)])
+def test_a_rolling_cache_resumed_from_its_window(Nq, window, sinks, spare, kv, dtype):
+    """A cache with room to spare that holds the sinks and the last windows only: the other rows were never written."""
+    say(f"resumed cache Nq={Nq} window={window} sinks={sinks} {dtype}")
+    B, H, Hk, d, slots = 2, 4, 2, 128, sinks + window + Nq - 1 + spare
+    q, k, v, _ = _inputs(B, H, Hk, Nq, slots, d, dtype, 21)
+    kv_lens = [kv, kv - 3]
+    want, _, cost = ref.window_attention(q, k, v, window, sinks, None, kv_lens, ring=True)
+    _hide(k, v, Nq, window, sinks, None, kv_lens, ring=True)
+    out = sb.salad_window_attn_fwd(q, k, v, window, sinks, kv_lens=_lens(kv_lens), ring=True)
+    err = (out.double() - want).abs()
+    assert (err <= _bound_out(want, cost, dtype, d, slots)).all(), float(err.max())
+
+
+@pytest.mark.gpu
+@BOTH
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_without_keys_do_not_reach_the_gradients(d, dtype):
+    """Fewer keys than queries: the first queries see nothing, so what they and their dout hold reaches no gradient."""
+    say(f"queries without keys d={d} {dtype}")
+    B, H, Hk, Nq, Nk, window, sinks, kv_lens = 2, 4, 2, 150, 150, 40, 4, [100, 37]
+    q, k, v, dout = _inputs(B, H, Hk, Nq, Nk, d, dtype, 22)
+    out, lse, kl = torch.empty_like(q), torch.empty(B, H, Nq, device="cuda"), _lens(kv_lens)
+    sb.salad_window_attn_fwd(q, k, v, window, sinks, kv_lens=kl, out=out, lse=lse)
+    clean = [torch.zeros_like(t) for t in (q, k, v)]
+    sb.salad_window_attn_bwd(q, k, v, out, lse, dout, window, sinks, kv_lens=kl, dq=clean[0], dk=clean[1], dv=clean[2])
+    for b, kv in enumerate(kv_lens):
+        q[b, :, :Nq - kv], dout[b, :, :Nq - kv] = math.inf, math.nan
+    grads = [torch.zeros_like(t) for t in (q, k, v)]
+    sb.salad_window_attn_bwd(q, k, v, out, lse, dout, window, sinks, kv_lens=kl, dq=grads[0], dk=grads[1], dv=grads[2])
+    assert all(torch.equal(x, y) for x, y in zip(grads, clean))
