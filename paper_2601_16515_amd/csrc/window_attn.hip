@@ -255,17 +255,19 @@ __global__ __launch_bounds__(256, 2) void window_step_kernel(WindowArgs a, int r
     const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
     const int rt = rest % row_tiles, bk = rest / row_tiles, b = bk / a.Hk, hk = bk - b * a.Hk, G = a.H / a.Hk;
     const WindowSpan sp = window_span(a, b);
+    if (sp.qlen == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hh = lane >> 5;
     const int R = G * a.Nq, idx = rt * STEP_ROWS + l32, row = idx < R ? idx : R - 1;
-    const int n = row % a.Nq, h = hk * G + row / a.Nq;
-    const bool live = idx < R && n < sp.qlen;
+    const int tok = row % a.Nq, h = hk * G + row / a.Nq;
+    const bool live = idx < R && tok < sp.qlen;
+    const int n = min(tok, sp.qlen - 1);        // the rows of a wave share the choice of a new reference: what lies behind the last has no say in it
     const u16 *kb = reinterpret_cast<const u16 *>(a.k) + (size_t)bk * a.Nk * D;
     const u16 *vb = reinterpret_cast<const u16 *>(a.v) + (size_t)bk * a.Nk * D;
     const size_t orow = ((size_t)b * a.H + h) * a.Nq + n;
     const int p = sp.off + n;
 
     const int first = window_first(a, sp.off);
-    const KeyTiles tiles(a, sp.off, sp.qlen > 0 ? sp.kv - 1 : -1, 32);
+    const KeyTiles tiles(a, sp.off, sp.kv - 1, 32);
     const int t0 = (int)((long long)tiles.n * split / a.splits), t1 = (int)((long long)tiles.n * (split + 1) / a.splits);
 
     Frag qf[NS];
@@ -476,11 +478,12 @@ __global__ __launch_bounds__(256, 2) void window_f32_kernel(WindowArgs a, int ro
     __shared__ float msh[4][16], lsh[4][16];
     const int rt = blockIdx.x % row_tiles, bk = blockIdx.x / row_tiles, b = bk / a.Hk, hk = bk - b * a.Hk, G = a.H / a.Hk;
     const WindowSpan sp = window_span(a, b);
+    if (sp.qlen == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int R = G * a.Nq, first = rt * 16, last = min(first + 15, R - 1);
     const int idx = first + i, row = idx < R ? idx : R - 1;
-    const int n = row % a.Nq, h = hk * G + row / a.Nq;
-    const bool live = idx < R && n < sp.qlen;
+    const int tok = row % a.Nq, n = min(tok, sp.qlen - 1), h = hk * G + row / a.Nq;
+    const bool live = idx < R && tok < sp.qlen;
     const size_t orow = ((size_t)b * a.H + h) * a.Nq + n;
     const int p = sp.off + n;
     // positions of the tile's rows: a range, or all of them where it holds rows of two heads

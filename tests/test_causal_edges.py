@@ -97,3 +97,23 @@ def test_queries_without_keys_do_not_reach_the_gradients(d, dtype):
     grads = [torch.zeros_like(t) for t in (q, k, v)]
     sb.salad_window_attn_bwd(q, k, v, out, lse, dout, window, sinks, kv_lens=kl, dq=grads[0], dk=grads[1], dv=grads[2])
     assert all(torch.equal(x, y) for x, y in zip(grads, clean))
+
+
+@pytest.mark.gpu
+@BOTH
+@pytest.mark.parametrize("B,H,Hk,Nq,Nk,window,sinks", [(8, 64, 64, 4, 1600, 1500, 4), (4, 128, 32, 16, 1200, 1100, 0), (1, 8, 1, 16, 4100, 4000, 130)])
+def test_what_lies_behind_a_samples_queries_changes_no_bit(B, H, Hk, Nq, Nk, window, sinks, dtype):
+    """The same call, twice, with small and with large finite values in the padding."""
+    say(f"padding B={B} H={H} Nq={Nq} {dtype}")
+    q, k, v, _ = _inputs(B, H, Hk, Nq, Nk, 64, dtype, 23)
+    q_lens = [1 + (3 * b + 1) % Nq for b in range(B)]
+    got = []
+    for size in (0.0, 1.0, 60.0):
+        x = q.clone()
+        for b, n in enumerate(q_lens):
+            x[b, :, n:] *= size
+        out, lse = torch.zeros_like(q), torch.zeros(B, H, Nq, device="cuda")
+        sb.salad_window_attn_fwd(x, k, v, window, sinks, q_lens=_lens(q_lens), out=out, lse=lse)
+        got.append((out, lse))
+    for out, lse in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
