@@ -431,12 +431,16 @@ static void launch_delta_rows(const WindowArgs &a, hipStream_t st)
     else launch_kernel((window_delta_kernel<T, 64>), grid, dim3(256), 0, st, a, rows);
 }
 
-// Keys among the sinks are seen by every later query, the others by `window` of them: their queries are cut into pieces of about as many.
+// Keys among the sinks are seen by every later query, the others by `window` of them: their queries are cut into pieces of about as many, as
+// long as the pieces of the call are no more than 8 for each of the 256 compute units.  More would balance nothing, and each costs 2 D x 128
+// floats of scratch (at most 256 MiB in all).  N = 12480, window 300, 1560 sinks, d = 128, without that end and with it: 12 heads 1044 (30 pieces) and
+// 921 us (13), 96 heads 7709 (30) and 6302 (1); 12 heads, all keys sinks, window 16: 6782 (64) and 2856 (1).
 int window_sink_pieces(const WindowArgs &a)
 {
-    if (!window_sink_tiles_of(a)) return 1;
+    const long long tiles = (long long)a.B * a.Hk * window_sink_tiles_of(a);
+    if (!tiles) return 1;
     const long long one = (long long)a.window + 128;
-    return (int)std::min(64ll, std::max(1ll, (a.Nq + one - 1) / one));
+    return (int)std::max(1ll, std::min({64ll, (a.Nq + one - 1) / one, 2048 / tiles}));
 }
 
 hipError_t launch_window_bwd_bf16(const WindowArgs &a, hipStream_t st)

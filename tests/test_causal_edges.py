@@ -1,4 +1,5 @@
 """The causal operators where their calls end: rows that nobody sees, rows behind a sample's last, calls that fill the chip."""
+import ctypes as C
 import math
 
 import pytest
@@ -117,3 +118,19 @@ def test_what_lies_behind_a_samples_queries_changes_no_bit(B, H, Hk, Nq, Nk, win
         got.append((out, lse))
     for out, lse in got[1:]:
         assert torch.equal(out, got[0][0]) and torch.equal(lse, got[0][1])
+
+
+@pytest.mark.parametrize("B,H,Hk,N,d,window,sinks", [
+    (1, 12, 12, 12480, 128, 16, 12480),      # plain causal attention, all keys among the sinks
+    (1, 12, 12, 32760, 128, 16, 1 << 30),
+    (8, 12, 12, 12480, 128, 300, 1560),
+    (64, 64, 64, 512, 64, 1, 512),
+    (1, 12, 12, 12480, 128, 4680, 1560), (1, 1, 1, 32760, 128, 1, 4), (1, 2, 1, 32760, 64, 64, 32760),
+])
+def test_scratch_of_the_sinks_gradients_is_bounded(B, H, Hk, N, d, window, sinks):
+    """Besides a float a query row: no more partial sums than fill the chip, 256 MiB (and 256 bytes for each part's alignment)."""
+    p = sb.WindowParams()
+    for n, x in dict(B=B, H=H, Hk=Hk, Nq=N, Nk=N, d=d, dtype=sb.SALAD_BF16, window=window, sinks=sinks).items():
+        setattr(p, n, x)
+    need = sb.lib().salad_window_attn_workspace_bytes(C.byref(p), 1)
+    assert 4 * B * H * N <= need <= 4 * B * H * N + (1 << 28) + 512, need
