@@ -442,12 +442,14 @@ def salad_tune(key: str, value: int) -> None:
 # ---------------------------------------------------------------------------------------------
 
 class CausalWorkspace:
-    """Scratch for the calls of a causal layer on one stream.  It grows to the largest call that it is passed to (or to `nbytes` at
-    once); a call that is captured into a graph has to find it large enough, so run the call once before, and keep the object as
-    long as the graph.  Calls that may overlap must not share one."""
+    """Scratch for the calls of a causal layer on one stream.  It grows to the largest call that it is passed to, by a quarter at least (or is
+    made with `nbytes` at once); a call that is captured into a graph has to find it large enough, so run the call once before, and
+    keep the object as long as the graph: a buffer that a graph was captured with stays when a larger one takes its place, others
+    go back.  Calls that may overlap must not share one."""
 
     def __init__(self, nbytes: int = 0, device=None):
         self.buf, self.kept, self.ptr, self.bytes = None, [], 0, 0
+        self.captured, self.stream = False, None        # of the present buffer: whether a graph uses it; the stream it was last handed to
         if nbytes:
             import torch
             self._grow(int(nbytes), torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device))
@@ -456,10 +458,21 @@ class CausalWorkspace:
         import torch
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError(f"the workspace has {self.bytes} bytes and a captured call needs {need}: run the call once before its capture")
-        if self.buf is not None:
-            self.kept.append(self.buf)              # graphs that were captured with it go on using it
+        if self.captured:
+            self.kept.append(self.buf)
+        need = max(need, self.bytes + self.bytes // 4)  # lengths that rise call by call do not allocate every time
+        self.buf, self.captured, self.stream = None, False, None
         self.buf = torch.empty(need + 256, dtype=torch.uint8, device=device)
         self.ptr, self.bytes = (self.buf.data_ptr() + 255) & ~255, need
+
+    def handed(self, stream: int) -> None:
+        """Notes a call on `stream`, the current one, that has the buffer."""
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            self.captured = True
+        elif stream != self.stream:
+            self.buf.record_stream(torch.cuda.current_stream(self.buf.device))      # it may have been allocated on another
+            self.stream = stream
 
     def room(self, need: int, device):
         """(pointer, bytes) for a call that needs `need` bytes."""
@@ -526,9 +539,12 @@ def _run(index, make, fn, need, backward, workspace):
             ptr, have = 0, 0
     else:
         ptr, have = ws.ptr, ws.bytes
+    if ws is not None and ws.buf is not None and not (ws.captured and ws.stream == stream):
+        ws.handed(stream)
     st = fn(pack(*args, ptr, have, stream))
     if st == SALAD_ENOSPC and ws is not None:
         ptr, have = ws.room(int(need(pack(*args, 0, 0, stream), backward)), torch.device("cuda", index))
+        ws.handed(stream)
         st = fn(pack(*args, ptr, have, stream))
     _check(st)
     return result

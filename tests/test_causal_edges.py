@@ -134,3 +134,75 @@ def test_scratch_of_the_sinks_gradients_is_bounded(B, H, Hk, N, d, window, sinks
         setattr(p, n, x)
     need = sb.lib().salad_window_attn_workspace_bytes(C.byref(p), 1)
     assert 4 * B * H * N <= need <= 4 * B * H * N + (1 << 28) + 512, need
+
+
+def test_a_workspace_keeps_what_graphs_use_and_nothing_else(monkeypatch):
+    capturing = False
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    ws, cpu = sb.CausalWorkspace(), torch.device("cpu")
+    buffers = set()
+    for need in range(1000, 101000, 1000):
+        ptr, have = ws.room(need, cpu)
+        assert have >= need and ptr % 256 == 0 and ws.buf.data_ptr() <= ptr and ptr + have <= ws.buf.data_ptr() + ws.buf.numel()
+        buffers.add(ptr)
+    assert not ws.kept and len(buffers) <= 24, (len(ws.kept), len(buffers))         # 1.25^21 > 100
+    capturing = True
+    ws.handed(0)
+    with pytest.raises(RuntimeError, match="before its capture"):
+        ws.room(10 * have, cpu)
+    capturing = False
+    graph_buffer = ws.buf
+    for need in (have + 1, 2 * have, 4 * have):
+        ws.room(need, cpu)
+    assert len(ws.kept) == 1 and ws.kept[0] is graph_buffer and ws.buf is not graph_buffer
+
+
+@pytest.mark.gpu
+def test_a_workspace_that_grows_between_graphs_and_streams():
+    """Rising lengths hold one buffer; a graph that was captured with an outgrown one still runs; a buffer that goes back while
+    another stream than its own works in it is not given out before that stream is done."""
+    say("workspace that grows")
+    d, window, sinks = 64, 100, 8
+    ws = sb.CausalWorkspace()
+
+    def inputs(N):
+        q, k, v, dout = _inputs(1, 2, 1, N, N, d, torch.bfloat16, 24)
+        out, lse = torch.empty_like(q), torch.empty(1, 2, N, device="cuda")
+        sb.salad_window_attn_fwd(q, k, v, window, sinks, out=out, lse=lse)
+        return q, k, v, out, lse, dout
+
+    small = inputs(300)
+    want = sb.salad_window_attn_bwd(*small, window, sinks)
+    got = [torch.zeros_like(t) for t in want]
+    run = lambda: sb.salad_window_attn_bwd(*small, window, sinks, dq=got[0], dk=got[1], dv=got[2], workspace=ws)  # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    assert ws.captured
+    for N in range(400, 2000, 200):
+        sb.salad_window_attn_bwd(*inputs(N), window, sinks, workspace=ws)
+    assert len(ws.kept) == 1 and not ws.captured
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    # allocated on one stream, used on another, outgrown there while that one is busy
+    x, side = inputs(1000), torch.cuda.Stream()
+    need = ws.bytes
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    ws = sb.CausalWorkspace(64 << 20)
+    assert need < ws.bytes
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sb.salad_window_attn_bwd(*x, window, sinks, workspace=ws)
+        torch.cuda._sleep(200_000_000)
+        old = ws.buf.data_ptr()
+        ws.room(65 << 20, torch.device("cuda", torch.cuda.current_device()))
+    other = torch.empty((64 << 20) + 256, dtype=torch.uint8, device="cuda")
+    busy = not side.query()
+    torch.cuda.synchronize()
+    assert not busy or other.data_ptr() != old
