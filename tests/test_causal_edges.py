@@ -206,3 +206,14 @@ def test_a_workspace_that_grows_between_graphs_and_streams():
     busy = not side.query()
     torch.cuda.synchronize()
     assert not busy or other.data_ptr() != old
+
+
+def test_a_workspace_stays_on_its_device(monkeypatch):
+    """Whether it is large enough or not.  (The devices here are ones that need no GPU.)"""
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    ws = sb.CausalWorkspace()
+    ptr, _ = ws.room(1000, torch.device("cpu"))
+    for need in (0, 500, 1000, 1001, 100000):
+        with pytest.raises(ValueError, match="the workspace is on cpu"):
+            ws.room(need, torch.device("meta"))
+    assert ws.room(1000, torch.device("cpu")) == (ptr, 1000) and not ws.kept
