@@ -445,7 +445,7 @@ class CausalWorkspace:
     """Scratch for the calls of a causal layer on one stream.  It grows to the largest call that it is passed to, by a quarter at least (or is
     made with `nbytes` at once); a call that is captured into a graph has to find it large enough, so run the call once before, and
     keep the object as long as the graph: a buffer that a graph was captured with stays when a larger one takes its place, others
-    go back.  Calls that may overlap must not share one."""
+    go back.  It stays on the device of its first buffer.  Calls that may overlap must not share one."""
 
     def __init__(self, nbytes: int = 0, device=None):
         self.buf, self.kept, self.ptr, self.bytes = None, [], 0, 0
@@ -476,10 +476,10 @@ class CausalWorkspace:
 
     def room(self, need: int, device):
         """(pointer, bytes) for a call that needs `need` bytes."""
+        if self.buf is not None and self.buf.device != device:
+            raise ValueError(f"the workspace is on {self.buf.device}, the call's tensors are on {device}")
         if need > self.bytes:
             self._grow(need, device)
-        elif self.buf is not None and self.buf.device != device:
-            raise ValueError(f"the workspace is on {self.buf.device}, the call's tensors are on {device}")
         return self.ptr, self.bytes
 
 
