@@ -461,7 +461,7 @@ class CausalWorkspace:
         if self.captured:
             self.kept.append(self.buf)
         need = max(need, self.bytes + self.bytes // 4)  # lengths that rise call by call do not allocate every time
-        self.buf, self.captured, self.stream = None, False, None
+        self.buf, self.ptr, self.bytes, self.captured, self.stream = None, 0, 0, False, None
         self.buf = torch.empty(need + 256, dtype=torch.uint8, device=device)
         self.ptr, self.bytes = (self.buf.data_ptr() + 255) & ~255, need
 

@@ -217,3 +217,20 @@ def test_a_workspace_stays_on_its_device(monkeypatch):
         with pytest.raises(ValueError, match="the workspace is on cpu"):
             ws.room(need, torch.device("meta"))
     assert ws.room(1000, torch.device("cpu")) == (ptr, 1000) and not ws.kept
+
+
+def test_a_workspace_whose_growth_failed_is_empty(monkeypatch):
+    """The old buffer went back for the larger one: nothing may be handed out from it."""
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    ws, cpu = sb.CausalWorkspace(), torch.device("cpu")
+    ws.room(1000, cpu)
+
+    def none_left(*args, **kw):
+        raise RuntimeError("out of memory")
+    with monkeypatch.context() as m:
+        m.setattr(torch, "empty", none_left)
+        with pytest.raises(RuntimeError, match="out of memory"):
+            ws.room(5000, cpu)
+    assert ws.buf is None and ws.ptr == 0 and ws.bytes == 0
+    ptr, have = ws.room(500, cpu)
+    assert ws.buf.data_ptr() <= ptr and ptr + have <= ws.buf.data_ptr() + ws.buf.numel()
