@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256) void window_append_kernel(AppendArgs a, long l
     const int b = (int)(bk / a.Hk);
     int ql = a.q_lens ? a.q_lens[b] : a.Nq;
     ql = ql < 0 ? 0 : ql > a.Nq ? a.Nq : ql;
-    const int kv = min(a.kv_lens[b], WINDOW_MAX_POSITION), p = kv - ql + n;
+    const int kv = min(max(a.kv_lens[b], 0), WINDOW_MAX_POSITION), p = kv - ql + n;    // lengths are device data, as in window_span
     if (n >= ql || p < 0) return;
     int row = p;
     if (a.ring && p >= a.sinks) {

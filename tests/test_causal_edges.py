@@ -234,3 +234,21 @@ def test_a_workspace_whose_growth_failed_is_empty(monkeypatch):
     assert ws.buf is None and ws.ptr == 0 and ws.bytes == 0
     ptr, have = ws.room(500, cpu)
     assert ws.buf.data_ptr() <= ptr and ptr + have <= ws.buf.data_ptr() + ws.buf.numel()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ring", [True, False])
+def test_append_of_lengths_out_of_range(ring):
+    """Lengths below zero are none, tokens before position 0 are left out, a length past 2^30 is 2^30."""
+    say(f"append lengths ring={ring}")
+    B, Hk, N, d, sinks, slots = 5, 2, 4, 64, 3, 23
+    _, k, v, _ = _inputs(B, Hk, Hk, N, N, d, torch.bfloat16, 25)
+    kc, vc = (torch.full((B, Hk, slots, d), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    want_k, want_v = kc.clone(), vc.clone()
+    sb.salad_window_cache_append(k, v, kc, vc, sinks, _lens([-2 ** 31, -1, 2, 2 ** 31 - 1, 9]), q_lens=_lens([N, N, 2 ** 31 - 1, N, -5]), ring=ring)
+    want_k[2, :, :2], want_v[2, :, :2] = k[2, :, 2:], v[2, :, 2:]
+    if ring:
+        for n in range(N):
+            row = sinks + (2 ** 30 - N + n - sinks) % (slots - sinks)
+            want_k[3, :, row], want_v[3, :, row] = k[3, :, n], v[3, :, n]
+    assert torch.equal(kc, want_k) and torch.equal(vc, want_v)
