@@ -262,7 +262,8 @@ salad_status salad_gate_fwd_static(const void *x_t, const float *w_gate, float b
  *                     sinks + (j - sinks) % (Nk - sinks).  kv_lens is then needed, counts all positions ever (up to 2^30), and
  *                     Nk >= sinks + window + Nq - 1 is needed for every key that some query sees to be there still.
  * A value that is not finite in a key or value row reaches the queries that see the row, and may reach queries close to them that
- * do not (0 * NaN in a shared tile).
+ * do not (0 * NaN in a shared tile); backward the same of a query's rows and the keys that it sees.
+ * Scores (scale q.k) may reach 2^29 in magnitude.  The gradients' P is off by |lse| 2^-24 of itself, since lse is fp32.
  * bf16: matrix cores, fp32 accumulation, P (and dS) rounded to bf16 for the products.  fp32: fp32 matrix instructions.
  * Results do not depend on what else runs: no atomics, the same bits for the same call. */
 typedef struct salad_window_params {
@@ -302,8 +303,9 @@ salad_status salad_window_cache_append(const void *k_new, const void *v_new, voi
                                        const int32_t *q_lens, const int32_t *kv_lens, void *hip_stream);
 
 /* ---- causal layers: gated delta rule -------------------------------------------------------------
- * The recurrent, causal counterpart of the layer's linear branch: a state S [d, d] per head (key channel, value channel) that
- * forgets by a gate and writes by the delta rule,
+ * Causal linear attention with a state that forgets and corrects itself, beside window attention what the linear branch is beside the sparse
+ * one; it is no recurrent form of that branch, whose feature map and normaliser it does not have.  A state S [d, d] per head (key channel,
+ * value channel) forgets by a gate and is written by the delta rule,
  *   u_t = beta_t (v_t - e^g_t S_{t-1}^T k_t),   S_t = e^g_t S_{t-1} + k_t u_t^T,   out_t = scale S_t^T q_t.
  *   q, k [B,Hk,N,d], v, out [B,H,N,d], H a multiple of Hk: value head h reads query and key head h / (H / Hk).  d is 64 or 128.
  *   g, beta    fp32 [B,H,N]: logarithm of the decay (0 keeps, -infinity forgets all) and writing strength.  The state stays bounded

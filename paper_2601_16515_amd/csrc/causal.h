@@ -1,5 +1,5 @@
 // Internal declarations of the causal layer's operators: window attention with sinks (window_attn.hip, window_grad.hip) and the
-// gated delta rule (delta_step.hip, delta_chunk.hip, delta_grad.hip).  Host side: causal_api.hip.
+// gated delta rule (delta_step.hip, delta_chunk.hip, delta_chain.hip, delta_grad.hip).  Host side: causal_api.hip.
 #pragma once
 #include "salad_internal.h"
 

@@ -487,8 +487,14 @@ __global__ __launch_bounds__(256) void delta_start_kernel(DeltaArgs a, int block
 
 // Groups: as many as shorten the passes.  One pass of all chunks without groups; with G groups one of a G-th for B and M, and one
 // of a G-th for the rest, each as often as its workgroups fill the chip's 256 compute units; 4 chunks of time for a step of the start kernel.
-// 12 heads, 512 chunks, d = 128: 1303 us in one group, 244 + 20 + 269 in groups.  Fewer than 8 chunks a group, or less than a fifth
-// to win, leave one group: the sum and start kernels cost that much.
+// Fewer than 8 chunks a group, or less than a fifth to win, leave one group: the sum and start kernels cost that much.
+// Whole calls, us, in one group, as the rule cuts them, and at best (groups):
+//   12 heads, d = 128   forward, 512 chunks 1490 591 (6) 564 (10),  64 chunks 189 120 (5) 116 (6);   backward, 195 chunks 1189 825 (4) 812 (10)
+//   40 heads, d = 128   forward, 256 chunks 870 870 (1) 834 (3);                                     backward 2862 2862 (1) 2862 (1)
+//   64 heads, d = 64    forward, 64 chunks 181 181 (1) 164 (3);                                      backward 613 612 (1) 610 (2)
+//   4 heads, d = 128    forward, 32 chunks 96 96 (1) 73 (4);                                         backward 178 178 (1) 129 (8)
+//   2 heads, d = 64     forward, 55 chunks 120 66 (5) 56 (8);                                        backward 194 108 (5) 91 (10)
+// So it is within 5 % of the best for many chunks; short sequences of few heads would take more groups than it gives them.
 int delta_groups(const DeltaArgs &a, bool backward)
 {
     const int parts = a.D / (a.bf16 ? 64 : 32);

@@ -5,7 +5,10 @@
 //   S_new^T q = e^g S^T q + (q.k) u,
 // so that a token costs one pass over the registers and one exchange through LDS.  Bound by reading and writing the state once
 // (8 D^2 bytes a head).  Many heads: all columns in one workgroup, rows of 512 bytes, past the caches (128 samples, 40 heads, d = 128:
-// 113.8 us = 5.93 TB/s; 118.2 through the caches, 122.4 with 64 columns a workgroup).  Few heads: 16 columns, for more workgroups.
+// 113.8 us = 5.93 TB/s; 118.2 through the caches, 122.4 with 64 columns a workgroup).  Fewer than 512 heads: 16 columns, for more workgroups.
+// In a graph, whole rows and 16 columns, us: d = 128, one token 12 heads 3.8 and 3.2, 32 heads 3.9 and 4.0, 128 heads 4.6 and 8.5, 512 heads 8.6 and
+// 20.7; 32 tokens 12 heads 38 and 32, 64 heads 39 and 42, 256 heads 41 and 131.  d = 64, one token 12 heads 2.8 and 2.9, 512 heads 3.9 and
+// 9.9.  So 16 columns win below some 40 heads of 128 alone, by a sixth, and the bound of 512 is too far out.
 #include <algorithm>
 
 #include "causal.h"
@@ -83,6 +86,9 @@ __global__ __launch_bounds__(256, 2) void delta_step_kernel(DeltaArgs a)
         }
 }
 
+// Up to 32 tokens, as the interface says (what a value that is not finite may reach changes there).  Token by token and in a chunk, us: 12 heads,
+// d = 128 8 tokens 10.1 and 16.4, 14 15.1 and 15.4, 32 32.0 and 16.4; 5120 heads 8 tokens 153 and 350, 24 314 and 357, 32 395 and 361;
+// 64 heads, d = 64 14 tokens 14.4 and 14.3, 32 30.0 and 15.3.  They cross at 14 tokens for few heads and at 28 for many.
 bool delta_takes_step(const DeltaArgs &a) { return a.N <= 32; }
 
 template <typename T, int D>

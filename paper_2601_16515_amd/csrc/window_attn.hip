@@ -234,8 +234,11 @@ static void launch_fwd(const WindowArgs &a, hipStream_t st)
 
 hipError_t launch_window_fwd_bf16(const WindowArgs &a, hipStream_t st)
 {
-    // 8 waves share a tile of K and V where that leaves two workgroups for each compute unit: 12 heads, N = 32760, d = 128 1677 -> 1593 us.  At
-    // d = 64 a workgroup of 4 leaves room for a third beside it, and 8 are slower (164 -> 205 us at 24 heads, N = 4095).
+    // 8 waves share a tile of K and V where that leaves two workgroups for each compute unit.  d = 128, 4 and 8 waves: 12 heads, window 6240, 1560
+    // sinks, N = 32760 1501 and 1411 us, N = 16384 (768 workgroups) 701 and 686, N = 10922 (516) 458 and 469, N = 2048 49 and 59.  Short
+    // windows lose by it at any size, which the rule does not ask: 48 heads, N = 8190, window 500 185 and 198, 24 heads, N = 32760, window 300 293 and
+    // 330 (every wave waits at the edge tiles of 256 queries).  d = 64: 4 waves leave room for a third workgroup, and 8 are slower (24 heads,
+    // N = 4095, window 1000 144 and 183; 12 heads, N = 32760, window 6240 868 and 947).
     if (a.D == 128 && (long long)a.B * a.H * ((a.Nq + 255) / 256) >= 512) launch_fwd<128, 8>(a, st);
     else if (a.D == 128) launch_fwd<128, 4>(a, st);
     else launch_fwd<64, 4>(a, st);
@@ -450,6 +453,11 @@ int window_step_splits(int B, int Hk, int row_tiles, int max_keys)
     return (int)std::max(1ll, std::min({std::max(want, even), most, 64ll}));
 }
 
+// Up to 16 queries a sample go with the keys in shares, more by tiles of 128 queries, each over all its keys.  Here and by tiles, us:
+//   12 heads, window 6240, 1560 sinks, d = 128:             1 query 32 and 173,   16 33 and 174,    64 34 and 177
+//   64 samples, 40 heads on 8, window 4096, 4 sinks:        1 query 195 and 1205, 16 355 and 1235,  64 990 and 1268
+//   4 samples, 24 heads on 8, window 1000, 4 sinks, d = 64: 1 query 11 and 21,    16 13 and 23,     64 20 and 24
+// So the two cross past 64 queries, and 17 to 64 would be faster here, too.
 bool window_takes_step(const WindowArgs &a) { return a.Nq <= 16; }
 
 hipError_t launch_window_step_bf16(const WindowArgs &a, hipStream_t st)

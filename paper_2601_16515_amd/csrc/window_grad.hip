@@ -10,8 +10,9 @@
 //   acc1^T += Y1^T dS,  acc2^T += Y2^T P      (dq;   dk and dv)
 // without leaving the registers.  Each own row's sum runs over the streamed rows in order: no atomics, the same bits every time.
 // P and dS are rounded to bf16 for the products (half a step, 2^-9, as the results are); sums and accumulators are fp32.
-// 12 heads, N = 12480, d = 128: keys 1361 us, queries 720 us (fastest 1255, 683).  The keys' workgroup reads each streamed tile from LDS as often as the matrix
-// cores need its products, so both take the same time, and its accumulators leave one wave to a SIMD to overlap them.
+// 12 heads, N = 12480, d = 128, by the trace: keys 1333 us, queries 720 us (fastest 1246, 679).  The keys' workgroup reads each streamed tile
+// from LDS as often as the matrix cores need its products, so both take the same time, and its accumulators leave one wave to a SIMD to
+// overlap them.
 #include <algorithm>
 #include <type_traits>
 
@@ -434,7 +435,8 @@ static void launch_delta_rows(const WindowArgs &a, hipStream_t st)
 // Keys among the sinks are seen by every later query, the others by `window` of them: their queries are cut into pieces of about as many, as
 // long as the pieces of the call are no more than 8 for each of the 256 compute units.  More would balance nothing, and each costs 2 D x 128
 // floats of scratch (at most 256 MiB in all).  N = 12480, window 300, 1560 sinks, d = 128, without that end and with it: 12 heads 1044 (30 pieces) and
-// 921 us (13), 96 heads 7709 (30) and 6302 (1); 12 heads, all keys sinks, window 16: 6782 (64) and 2856 (1).
+// 921 us (13), 96 heads 7709 (30) and 6302 (1); 12 heads, all keys sinks, window 16: 6782 (64) and 2856 (1).  The same calls in one
+// piece: 12 heads 1039; with 4 sinks 907 (307 in the rule's 30), with window 4680 2197 (1938 in 3).
 int window_sink_pieces(const WindowArgs &a)
 {
     const long long tiles = (long long)a.B * a.Hk * window_sink_tiles_of(a);

@@ -252,3 +252,24 @@ def test_append_of_lengths_out_of_range(ring):
             row = sinks + (2 ** 30 - N + n - sinks) % (slots - sinks)
             want_k[3, :, row], want_v[3, :, row] = k[3, :, n], v[3, :, n]
     assert torch.equal(kc, want_k) and torch.equal(vc, want_v)
+
+
+@pytest.mark.gpu
+@BOTH
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("Nq", [3, 150])
+def test_scores_of_large_magnitude(Nq, sign, dtype):
+    """Scores up to 2^29 on either side of 0, exact in every type: rows are those of the largest keys, and lse is the largest score."""
+    say(f"large scores Nq={Nq} sign={sign} {dtype}")
+    B, H, N, d, window, sinks = 1, 2, 300, 64, 90, 5
+    g = torch.Generator(device="cuda").manual_seed(26)
+    q, k, v = torch.zeros(B, H, Nq, d, device="cuda"), torch.zeros(B, H, N, d, device="cuda"), torch.randn(B, H, N, d, generator=g, device="cuda")
+    q[..., 7] = sign * 2.0 ** 15
+    k[..., 7] = torch.randint(100, 256, (B, H, N), generator=g, device="cuda") * 2.0 ** 6
+    q, k, v = (x.to(dtype) for x in (q, k, v))
+    want, lse_want, cost = ref.window_attention(q, k, v, window, sinks, scale=1.0)
+    out, lse = torch.empty_like(q), torch.empty(B, H, Nq, device="cuda")
+    sb.salad_window_attn_fwd(q, k, v, window, sinks, softmax_scale=1.0, out=out, lse=lse)
+    assert ((out.double() - want).abs() <= _bound_out(want, cost, dtype, d, N)).all()
+    # lse: the reference in units of log 2, back in natural ones: four roundings of half a step
+    assert ((lse.double() - lse_want).abs() <= 4 * 2.0 ** -24 * lse_want.abs()).all()
