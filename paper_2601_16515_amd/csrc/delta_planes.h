@@ -2,7 +2,7 @@
 //
 // The state, u and their gradients are fp32 results of long recurrences, and their products have to keep that.  A float x is
 // x0 + x1 + x2 with x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1): 24 bits, exact but for values below the range.  The product
-// of three planes by three takes the six terms down to 2^-16 of the first (what is left out is below 2^-24), by a tensor that is bf16
+// of three planes by three takes the six terms down to 2^-16 of the first (what is left out adds up to 2^-23 of it at most), by a tensor that is bf16
 // already three.  The fp32 matrix instruction has a sixteenth of the bf16 rate: six products are 2.7 times faster, three 5.3 times.
 //
 // Lane l of an operand holds row l % 16 and the 8 contraction indices from 8 (l / 16) on; accumulator r is row 4 (l / 16) + r,

@@ -10,7 +10,7 @@
 //   window_f32_kernel    fp32
 // Both bf16 kernels compute S^T = K Q^T with the keys' rows permuted (kappa) so that the accumulators of 16 keys are, packed to bf16,
 // the B operand of O^T += V^T P^T as they stand: P never leaves the registers.  P is rounded to bf16 for that product (half a step,
-// 2^-9 relative, as the result itself is rounded to bf16); maxima, sums and accumulators are fp32.
+// 2^-8 relative at most, as the result itself is rounded to bf16); maxima, sums and accumulators are fp32.
 #include <algorithm>
 
 #include "causal.h"
