@@ -10,7 +10,8 @@
 //   dbeta_i = dR_i.v_i - gamma_i k_i.(dR S_0^T)_i + sum_j dA_ij e^(b_i - b_j) k_i.k_j,
 // and by the decays b_i: each term's product with what it decays, summed over rows (+) and columns (-); dg is the running sum of that
 // from the end of the chunk.  dg, dbeta and the state's gradient are fp32 results: their products keep fp32 (three planes).  The four
-// 64 x 64 x D products that reach only dq and dk take E and dP rounded to the tensors' type.
+// 64 x 64 x D products that reach only dq and dk take E and dP in two planes for bf16 tensors: with keys of nearly one direction the terms of dq are
+// 30 to 70 times their sum, and one plane left dq off by 1.1e-2, seven times its own rounding (now 1.7e-3, in 0.7 % more time of the call).
 #include <algorithm>
 
 #include "causal.h"
@@ -76,11 +77,11 @@ __global__ __launch_bounds__(256) void delta_x_kernel(DeltaArgs a)
 template <typename T, int D>
 __global__ __launch_bounds__(512, 1) void delta_grad_kernel(DeltaArgs a)
 {
-    constexpr int P = planes_of<T>(), NK = D / 32, NA = D / 32, SP = D + 8, UP = 72, SPL = 32 * SP, UPL = 32 * UP;
+    constexpr int P = planes_of<T>(), EP = out_planes<T>(), NK = D / 32, NA = D / 32, SP = D + 8, UP = 72, SPL = 32 * SP, UPL = 32 * UP;
     using Tile = Tile64<T, D>;
     extern __shared__ __attribute__((aligned(16))) u16 lds[];
     u16 *S0 = lds, *S1 = S0 + 3 * SPL, *Ut = S1 + 3 * SPL, *Rt = Ut + 3 * UPL;          // [32][D], [32][D], [32][64], [32][64]
-    u16 *X = lds, *Et = X + P * Tile::PLANE, *Pt = Et + P * 64 * UP;                    // afterwards: K or Q [64][D]; E and dP [token i][token j]
+    u16 *X = lds, *Et = X + P * Tile::PLANE, *Pt = Et + EP * 64 * UP;                    // afterwards: K or Q [64][D]; E and dP [token i][token j]
     __shared__ float cols[8][64], red[8], fin[2][64], fdb[2][64];
     const int ch = blockIdx.x % a.chunks, bh = blockIdx.x / a.chunks, b = bh / a.H, h = bh - b * a.H, G = a.H / a.Hk, hk = h / G;
     const int valid = min(delta_len(a, b) - ch * 64, 64);
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(512, 1) void delta_grad_kernel(DeltaArgs a)
                 rows += cs[r];
             }
         }
-        put4<P>((half == 0 ? Et : Pt) + tok * UP + 16 * x + 4 * l4, 64 * UP, e);
+        put4<EP>((half == 0 ? Et : Pt) + tok * UP + 16 * x + 4 * l4, 64 * UP, e);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float c = cs[r];
@@ -244,13 +245,13 @@ __global__ __launch_bounds__(512, 1) void delta_grad_kernel(DeltaArgs a)
         }
         if (lane < valid) a.dg[vrow0 + lane] = d;
     }
-    Op<P> en[2], pn[2], et[2], pt[2];
+    Op<EP> en[2], pn[2], et[2], pt[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-        en[kt] = frag_n<P>(Et, 64 * UP, UP, 16 * wave, 32 * kt, lane);
-        pn[kt] = frag_n<P>(Pt, 64 * UP, UP, 16 * wave, 32 * kt, lane);
-        et[kt] = frag_t<P>(Et, 64 * UP, UP, 16 * wave, 32 * kt, lane);
-        pt[kt] = frag_t<P>(Pt, 64 * UP, UP, 16 * wave, 32 * kt, lane);
+        en[kt] = frag_n<EP>(Et, 64 * UP, UP, 16 * wave, 32 * kt, lane);
+        pn[kt] = frag_n<EP>(Pt, 64 * UP, UP, 16 * wave, 32 * kt, lane);
+        et[kt] = frag_t<EP>(Et, 64 * UP, UP, 16 * wave, 32 * kt, lane);
+        pt[kt] = frag_t<EP>(Pt, 64 * UP, UP, 16 * wave, 32 * kt, lane);
     }
 #pragma unroll
     for (int x = 0; x < NA; ++x)
@@ -308,7 +309,7 @@ hipError_t run(const DeltaArgs &a, hipStream_t st)
 {
     constexpr int P = planes_of<T>(), tile = P * Tile64<T, D>::PLANE;
     constexpr int x_bytes = (tile + 3 * 64 * 72) * 2;
-    constexpr int blocks = 2 * 3 * 32 * (D + 8) + 2 * 3 * 32 * 72, pairs = tile + 2 * P * 64 * 72, grad_bytes = (blocks > pairs ? blocks : pairs) * 2;
+    constexpr int blocks = 2 * 3 * 32 * (D + 8) + 2 * 3 * 32 * 72, pairs = tile + 2 * out_planes<T>() * 64 * 72, grad_bytes = (blocks > pairs ? blocks : pairs) * 2;
     static bool dx[16], dg[16];
     if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_x_kernel<T, D>), x_bytes, dx)) return e;
     if (const hipError_t e = dyn_lds_attr_once(reinterpret_cast<const void *>(delta_grad_kernel<T, D>), grad_bytes, dg)) return e;

@@ -196,3 +196,38 @@ def test_a_call_for_another_device_switches_to_it_and_back(monkeypatch):
         return sb.SALAD_OK
     assert sb._run(1, make, fn, need, 0, None) == "result"
     assert seen == [("make", 1), ("need", 1, 101), ("call", 1, 101)] and now == [0]
+
+
+# ---- gated delta rule: gradients whose terms cancel --------------------------------------------------------
+
+def _terms_of_dq(q, k, v, g, beta, dout, state):
+    """Sums of the magnitudes of the terms of dq that come from the tokens of its chunk: scale e^(b_i - b_j) |dout_i.u_j| |k_j|, j <= i."""
+    B, Hk, N, d = q.shape
+    H = v.shape[1]
+    k, v, g, beta, dout = k.double().repeat_interleave(H // Hk, 1), v.double(), g.double(), beta.double(), dout.double()
+    S, u = torch.zeros(B, H, d, d, dtype=torch.float64, device=q.device) if state is None else state.double(), []
+    for t in range(N):
+        S = g[:, :, t, None, None].exp() * S
+        u.append(beta[:, :, t, None] * (v[:, :, t] - (k[:, :, t, None] @ S)[:, :, 0]))
+        S = S + k[:, :, t, :, None] * u[-1][:, :, None]
+    u, b, out = torch.stack(u, 2), g.cumsum(-1), torch.zeros(B, H, N, d, dtype=torch.float64, device=q.device)
+    for c in range(0, N, 64):
+        at = slice(c, min(c + 64, N))
+        ratio = torch.exp(b[:, :, at, None] - b[:, :, None, at]).tril()
+        out[:, :, at] = (ratio * (dout[:, :, at] @ u[:, :, at].transpose(-1, -2).contiguous()).abs()) @ k[:, :, at].abs() / math.sqrt(d)
+    return out.view(B, Hk, H // Hk, N, d).sum(2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,Hk,N,d,state", [(3, 2, 2, 57, 64, False), (2, 10, 2, 89, 128, False), (1, 2, 1, 64, 128, False), (2, 1, 1, 68, 64, True), (1, 3, 3, 200, 64, False)])
+def test_gradients_for_keys_of_nearly_one_direction(B, H, Hk, N, d, state):
+    """bf16.  The terms of dq are 25 to 70 times their sums.  Each result is rounded once (2^-8); E and dP have two planes, 2^-16 of a term."""
+    say(f"gradients of alike keys {B} {H} {Hk} {N} {d} {state}")
+    q, k, v, g, beta, S, dout = delta._inputs(B, H, Hk, N, d, torch.bfloat16, 34, state, "alike")
+    want = ref.gated_delta_gradients(q, k, v, g, beta, dout, S)
+    got = sb.salad_gated_delta_bwd(q, k, v, g, beta, dout, state=S)
+    terms = _terms_of_dq(q, k, v, g, beta, dout, S)
+    amount = float(terms.norm() / want[0].norm())
+    assert delta._rel(got[0], want[0]) < 2.0 ** -8 + 2.0 ** -16 * amount + delta._fp32(N, d, 16), (delta._rel(got[0], want[0]), amount)
+    for i in (1, 2):
+        assert delta._rel(got[i], want[i]) < 2.0 ** -8 + delta._fp32(N, d, 16), (delta.NAMES[i], delta._rel(got[i], want[i]))
