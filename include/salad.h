@@ -264,7 +264,8 @@ salad_status salad_gate_fwd_static(const void *x_t, const float *w_gate, float b
  * A value that is not finite in a key or value row reaches the queries that see the row, and may reach queries close to them that
  * do not (0 * NaN in a shared tile); backward the same of a query's rows and the keys that it sees.
  * Scores (scale q.k) may reach 2^29 in magnitude.  The gradients' P is off by |lse| 2^-24 of itself, since lse is fp32.
- * bf16: matrix cores, fp32 accumulation, P (and dS) rounded to bf16 for the products.  fp32: fp32 matrix instructions.
+ * bf16: matrix cores, fp32 accumulation, P (and dS) rounded to bf16 for the products: off by up to 2^-8 of the terms' magnitudes, which is more
+ * than 2^-8 of a sum whose terms cancel (gradients where keys are nearly alike).  fp32: fp32 matrix instructions.
  * Results do not depend on what else runs: no atomics, the same bits for the same call. */
 typedef struct salad_window_params {
     int32_t B, H, Hk, Nq, Nk, d;
@@ -316,7 +317,7 @@ salad_status salad_window_cache_append(const void *k_new, const void *v_new, voi
  * A value that is not finite reaches the state and so every later token of its sample and head; beyond 32 tokens also earlier ones of its
  * chunk of 64.
  * Up to 32 tokens go one after the other with the state in registers; more go in chunks of 64 on the matrix cores.  The
- * two agree up to rounding.  Everything in the chain of states is fp32, or split so that it keeps fp32's bits.  No atomics: the same bits for
+ * two agree up to rounding (bf16 in chunks: out takes the state before its chunk rounded to bf16).  Everything in the chain of states is fp32, or split so that it keeps fp32's bits.  No atomics: the same bits for
  * the same call. */
 typedef struct salad_delta_params {
     int32_t B, H, Hk, N, d;

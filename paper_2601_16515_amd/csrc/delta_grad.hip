@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void delta_x_kernel(DeltaArgs a)
 // ---- the rest, every chunk at once ----------------------------------------------------------------------------
 // Transposed: a lane's column is token i = 16 wave + l % 16, rows are key channels or the other token.  The contractions over the value
 // channels go in blocks of 32 through LDS, the next block on its way meanwhile.  8 waves: 4 of the tokens by 2 of the key channels; of the products
-// over pairs of tokens one half takes A's, the other P's.  12 heads, N = 12480, d = 128, bf16: 321 us (400 with 4 waves and blocks loaded
+// over pairs of tokens one half takes A's, the other P's.  12 heads, N = 12480, d = 128, bf16: 333 us (321 with E and dP in one plane; 400 with 4 waves and blocks loaded
 // when needed), bound by LDS: every plane of every operand is read from there by 8 waves, one workgroup to a compute unit.
 template <typename T, int D>
 __global__ __launch_bounds__(512, 1) void delta_grad_kernel(DeltaArgs a)
